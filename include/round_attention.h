@@ -14,6 +14,10 @@
  *   ra_watershed_attn_prefill     the same pass over the keys, the round scores (steps 2-3 fused)
  *   ra_round_sparse_attn_prefill  attention of the question's tokens over the selected rounds
  *                                 and, causally, over the question itself (step 4)
+ *   ra_round_sparse_attn_tree,    attention of a tree of drafted tokens over the selected rounds, and the accepted path moved
+ *   ra_tree_commit                behind the answer (not the paper's)
+ *   ra_token_weights,             attention weight of every token, the tokens to keep by it, and the smaller cache
+ *   ra_select_tokens, ra_compact_rounds   (not the paper's)
  *
  * Conventions
  * -----------
@@ -323,6 +327,113 @@ int ra_layer_divergence(ra_ctx* ctx, void* stream, const float* p, const int32_t
  */
 int ra_selection_coverage(ra_ctx* ctx, void* stream, const float* scores, const int32_t* sel_idx,
                           const int32_t* n_sel, int B, int R_max, float* coverage);
+
+/* ------------------------------------------------------------------------------------------
+ * Drafted tokens (speculative decoding): a draft model proposes a tree of tokens for every sequence, one pass of the model
+ * attends with all of them at once, the longest accepted path is kept.
+ * ------------------------------------------------------------------------------------------ */
+
+/*
+ * Round-sparse attention of a tree of drafted tokens (the decode call for several alternatives at once): node i of sequence
+ * b attends over the selected rounds of `layer`, the first cur_len[b] tokens of the current round (the question, the answer
+ * so far) and those nodes j of the tree whose bit is set in its row of `tree_mask` (its ancestors and, as a rule, itself).
+ * The nodes' own keys and values are in the current round's buffers behind the committed tokens, node j in row cur_len[b] + j.
+ *   q          device [B][n_nodes][Hq][d], dtype of the view
+ *   sel_idx, n_sel   as for ra_round_sparse_attn_decode
+ *   cur_k/v    device [B][cur_cap][Hkv][d], cur_cap >= n_nodes;  cur_len device int32 [B], the committed tokens WITHOUT the
+ *              tree (clamped to 0 .. cur_cap)
+ *   tree_mask  device uint32 [B][n_nodes][(n_nodes + 31) / 32]: bit j % 32 of word j / 32 of row i: node i sees node j.
+ *              Any relation is taken, not only a tree's; a node that sees nothing at all gets out = 0, lse = -inf
+ *   tree_len   device int32 [B] or NULL (= n_nodes): nodes of every sequence (clamped to 0 .. n_nodes, and to the rows left
+ *              in cur_k).  Nodes from there on get out = 0, lse = -inf, and their queries, keys and values are not used
+ *   out        device float [B][n_nodes][Hq][d];  lse device float [B][n_nodes][Hq] or NULL
+ * Values of rows that a node does not see are multiplied by zero: they must be finite.  bf16 and fp32, d = 64 or 128,
+ * Hq / Hkv <= 16.  q, keys, values, cur_k and out must be 16-byte aligned (RA_ERR_INVALID_ARG).
+ */
+int ra_round_sparse_attn_tree(ra_ctx* ctx, void* stream, const void* q, int n_nodes, int Hq, const ra_kv_view* layer,
+                              const int32_t* sel_idx, const int32_t* n_sel, const void* cur_k, const void* cur_v,
+                              const int32_t* cur_len, int cur_cap, const uint32_t* tree_mask, const int32_t* tree_len,
+                              float scale, float* out, float* lse);
+
+/*
+ * Commit of an accepted path: for every layer the keys and values of node path[b][j], in row cur_len[b] + path[b][j], move
+ * to row cur_len[b] + j, where the next step expects them, and new_len[b] = cur_len[b] + (nodes of the path).
+ *   cur_k_layers, cur_v_layers   host arrays of n_layers DEVICE pointers, each [B][cur_cap][Hkv][d], 16-byte aligned;
+ *              no two of them may overlap
+ *   cur_len    device int32 [B] (clamped to 0 .. cur_cap)
+ *   path       device int32 [B][max_path]: node indices in the order of the path.  A tree numbers its nodes behind their
+ *              parents, so path[b][j] >= j.  The path ends before the first entry that is smaller than j or whose row lies
+ *              outside cur_k, and after n_path[b] entries at the latest (device int32 [B], clamped to 0 .. max_path)
+ *   new_len    device int32 [B], another buffer than cur_len
+ * Rows behind the path keep what they held.  Needs Hkv * d * element size to be a multiple of 16 bytes
+ * (RA_ERR_UNSUPPORTED otherwise).  No workspace is used.
+ */
+int ra_tree_commit(ra_ctx* ctx, void* stream, void* const* cur_k_layers, void* const* cur_v_layers, int n_layers, int B,
+                   int cur_cap, int Hkv, int d, int dtype, const int32_t* cur_len, const int32_t* path,
+                   const int32_t* n_path, int max_path, int32_t* new_len);
+
+/* ------------------------------------------------------------------------------------------
+ * Eviction of single tokens by the attention they received: rounds shrink to the tokens that were attended to.  (Dropping
+ * whole rounds is ra_kv_store_drop_inactive.)  The position of a token is its index in its sequence's history, the rounds
+ * one after the other: token t of round r has position seg_len[0] + ... + seg_len[r - 1] + t.
+ * ------------------------------------------------------------------------------------------ */
+
+/*
+ * Attention weight that every history token received, added to a running total:
+ *   weights[b][p] = prev[b][p] + sum over query tokens i and heads h of exp(scale q_ih . k_p - lse[b][i][h])
+ * for the tokens of the selected rounds (every round with sel_idx = NULL; a round that the list names twice counts twice, as
+ * in the attention); other positions keep prev.  `lse` is what ra_round_sparse_attn_decode (q_len = 1), _prefill or _tree returned for the same
+ * q over the same selection.  A query row whose lse is not a finite number adds nothing (a node behind tree_len, an empty
+ * key set; a rejected node by setting its lse to infinity).
+ *   q          device [B][q_len][Hq][d], dtype of the view;  lse device float [B][q_len][Hq]
+ *   layer      only keys are read
+ *   prev       device float [B][n_pos] or NULL (zeros); may be `weights` itself, and must not overlap it otherwise
+ *   weights    device float [B][n_pos], wholly written; tokens at positions n_pos and above are left out
+ * bf16 and fp32, d = 64 or 128, Hq / Hkv <= 16.  q and keys must be 16-byte aligned (RA_ERR_INVALID_ARG).  No workspace
+ * is used.
+ */
+int ra_token_weights(ra_ctx* ctx, void* stream, const void* q, int q_len, int Hq, const ra_kv_view* layer,
+                     const int32_t* sel_idx, const int32_t* n_sel, const float* lse, float scale, const float* prev,
+                     float* weights, int n_pos);
+
+typedef struct ra_keep_params {
+    int32_t budget;     /* tokens to keep per sequence, >= 1, at least keep_first + keep_last       */
+    int32_t keep_first; /* the first tokens of the history are kept whatever their weight ...       */
+    int32_t keep_last;  /* ... and the last ones                                                    */
+    int32_t block_size; /* layout that kept_off is for: 0 (in tokens) or 16 (in block-table slots)   */
+    int64_t stride;     /* kept_off of sequence b starts at b * stride                              */
+} ra_keep_params;
+
+/*
+ * Choice of the tokens to keep: min(budget, tokens) of every sequence, the forced first and last ones and then those of
+ * the largest weight, ties to the lower position.
+ *   weights    device float [B][n_pos], not NaN;  positions n_pos and above count as not there
+ *   seg_len    device int32 [B][R_max], n_rounds device int32 [B]: those of the view
+ *   kept_idx   device int32 [B][budget]: positions of the kept tokens, ascending, -1 behind the last;  n_kept device int32 [B]
+ *   kept_len   device int32 [B][R_max]: tokens that every round keeps (0 from n_rounds[b] on): seg_len of the smaller cache
+ *   kept_off   device int64 [B][R_max] or NULL: a place for every round, packed in whole 16-token blocks behind b * stride,
+ *              in tokens (seg_off and seg_off_v of a contiguous cache) or slots (seg_off of a paged one)
+ *   kept_weights   device float [B][n_pos] or NULL: the kept tokens' weights at their new positions, 0 behind the last;
+ *              another buffer than `weights`
+ * n_pos <= 2^24.  No workspace is used.
+ */
+int ra_select_tokens(ra_ctx* ctx, void* stream, const float* weights, int n_pos, const int32_t* seg_len,
+                     const int32_t* n_rounds, int B, int R_max, const ra_keep_params* params, int32_t* kept_idx,
+                     int32_t* n_kept, int32_t* kept_len, int64_t* kept_off, float* kept_weights);
+
+/*
+ * The smaller cache: keys and values of the kept tokens of one layer, packed into round blocks of the new lengths.
+ *   src        the layer's view
+ *   kept_idx   device int32 [B][max_kept], ascending positions in src;  n_kept device int32 [B] (ra_select_tokens)
+ *   dst        view of the smaller cache: k and v (written; memory of their own, not overlapping src's), seg_off, seg_off_v,
+ *              seg_len = kept_len (adding up to n_kept), n_rounds, block_table.  B, R_max, Hkv, d and dtype of src; either
+ *              layout, whatever src's is
+ * Padding of the value tiles is zeroed; nothing outside the rounds' blocks is written.  With v NULL in both views only keys
+ * move.  A kept_idx entry that is no position of src's sequence gives zeros.  16-byte aligned storage
+ * (RA_ERR_INVALID_ARG).  No workspace is used.
+ */
+int ra_compact_rounds(ra_ctx* ctx, void* stream, const ra_kv_view* src, const int32_t* kept_idx, const int32_t* n_kept,
+                      int max_kept, const ra_kv_view* dst);
 
 /* ------------------------------------------------------------------------------------------
  * Round-indexed KV store for the post-watershed layers (Sec. 3.2: "u_m" lives in host memory as

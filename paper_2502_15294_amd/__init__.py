@@ -36,6 +36,7 @@ EXPORTS = [
     "ra_kv_store_release", "ra_kv_store_save_round", "ra_kv_store_save_wait", "ra_kv_store_round_activity",
     "ra_kv_store_drop_round", "ra_kv_store_drop_inactive",
     "ra_round_scores_accumulate", "ra_layer_divergence", "ra_selection_coverage", "ra_measure_read_bandwidth",
+    "ra_round_sparse_attn_tree", "ra_tree_commit", "ra_token_weights", "ra_select_tokens", "ra_compact_rounds",
 ]
 
 
@@ -49,6 +50,11 @@ class ra_select_params(C.Structure):
     _fields_ = [("strategy", C.c_int32), ("ddof", C.c_int32), ("min_rounds", C.c_int32), ("max_rounds", C.c_int32),
                 ("lambda_", C.c_double), ("fraction", C.c_double), ("threshold", C.c_double),
                 ("keep_first", C.c_int32), ("keep_last", C.c_int32)]
+
+
+class ra_keep_params(C.Structure):
+    _fields_ = [("budget", C.c_int32), ("keep_first", C.c_int32), ("keep_last", C.c_int32), ("block_size", C.c_int32),
+                ("stride", C.c_int64)]
 
 
 class ra_kv_view(C.Structure):
@@ -119,6 +125,18 @@ def lib() -> C.CDLL:
         L.ra_watershed_attn_prefill.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.POINTER(ra_kv_view),
                                                 C.c_void_p, C.c_void_p, C.c_int, C.c_float, C.c_void_p, C.c_void_p,
                                                 C.c_void_p, C.c_void_p]
+        L.ra_round_sparse_attn_tree.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.POINTER(ra_kv_view),
+                                                C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int,
+                                                C.c_void_p, C.c_void_p, C.c_float, C.c_void_p, C.c_void_p]
+        L.ra_tree_commit.argtypes = [C.c_void_p, C.c_void_p, C.POINTER(C.c_void_p), C.POINTER(C.c_void_p), C.c_int, C.c_int,
+                                     C.c_int, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int,
+                                     C.c_void_p]
+        L.ra_token_weights.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.POINTER(ra_kv_view),
+                                       C.c_void_p, C.c_void_p, C.c_void_p, C.c_float, C.c_void_p, C.c_void_p, C.c_int]
+        L.ra_select_tokens.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_int, C.c_int,
+                                       C.POINTER(ra_keep_params), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
+        L.ra_compact_rounds.argtypes = [C.c_void_p, C.c_void_p, C.POINTER(ra_kv_view), C.c_void_p, C.c_void_p, C.c_int,
+                                        C.POINTER(ra_kv_view)]
         L.ra_kv_store_create.argtypes = [C.POINTER(C.c_void_p), C.POINTER(ra_store_cfg)]
         L.ra_kv_store_destroy.argtypes = [C.c_void_p]
         L.ra_kv_store_register_round.argtypes = [C.c_void_p, C.c_int, C.c_int, C.c_void_p, C.c_int]
@@ -175,7 +193,8 @@ def _load_native():
     _binding.setup(_check, C.c_void_p, ra_kv_view, ra_select_params, _by_ctypes(C.CFUNCTYPE(C.c_void_p, C.c_void_p)(handle)),
                    _by_ctypes(C.CFUNCTYPE(C.c_float, C.c_float)(scale)), _WrongType, _NotATensor, *[C.cast(getattr(L, name), C.c_void_p).value for name in (
         "ra_round_scores", "ra_round_scores_select", "ra_round_scores_accumulate", "ra_selection_coverage",
-        "ra_round_sparse_attn_decode", "ra_watershed_attn_decode", "ra_round_sparse_attn_prefill", "ra_watershed_attn_prefill")])
+        "ra_round_sparse_attn_decode", "ra_watershed_attn_decode", "ra_round_sparse_attn_prefill", "ra_watershed_attn_prefill",
+        "ra_round_sparse_attn_tree", "ra_tree_commit", "ra_token_weights", "ra_select_tokens", "ra_compact_rounds")])
     _native = _binding
     return _native
 
@@ -397,6 +416,73 @@ def ra_watershed_attn_prefill(ctx, q: torch.Tensor, view: KVView, cur_k: Optiona
     """Returns (out, lse, scores_head, scores)."""
     return (_native or _load_native()).watershed_prefill(ctx, _stream(stream), q, view, cur_k, cur_v, scale, out, lse,
                                                          scores_head, scores)
+
+
+# ---- drafted tokens --------------------------------------------------------------------------------
+def make_tree_mask(parents) -> torch.Tensor:
+    """`tree_mask` of trees given by their nodes' parents, on the host: parents[b][i] is the parent of node i, a smaller index,
+    or -1 for a node right behind the committed tokens.  A node sees its ancestors and itself.  Shorter lists are padded with
+    nodes that see nothing.  Returns int32 [B, n_nodes, ceil(n_nodes / 32)]."""
+    n = max(len(p) for p in parents)
+    words = (n + 31) // 32
+    mask = torch.zeros((len(parents), n, words), dtype=torch.int32)
+    for b, tree in enumerate(parents):
+        sees = []
+        for i, parent in enumerate(tree):
+            if not -1 <= parent < i:
+                raise ValueError(f"node {i} of tree {b}: its parent {parent} is no smaller index")
+            sees.append((sees[parent] if parent >= 0 else 0) | 1 << i)
+            for w in range(words):
+                word = sees[i] >> 32 * w & 0xffffffff
+                mask[b, i, w] = word - (1 << 32) if word >> 31 else word
+    return mask
+
+
+def ra_round_sparse_attn_tree(ctx, q: torch.Tensor, view: KVView, tree_mask: torch.Tensor, cur_k: torch.Tensor,
+                              cur_v: torch.Tensor, cur_len: torch.Tensor, tree_len: Optional[torch.Tensor] = None,
+                              sel_idx: Optional[torch.Tensor] = None, n_sel: Optional[torch.Tensor] = None,
+                              scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
+                              lse: Optional[torch.Tensor] = None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """q [B, n_nodes, Hq, d]; tree_mask int32 [B, n_nodes, ceil(n_nodes / 32)] (make_tree_mask); the nodes' keys and values lie
+    in cur_k / cur_v [B, cur_cap, Hkv, d] from row cur_len[b] on.  Returns (out, lse)."""
+    return (_native or _load_native()).tree(ctx, _stream(stream), q, view, tree_mask, cur_k, cur_v, cur_len, tree_len, sel_idx,
+                                            n_sel, scale, out, lse)
+
+
+def ra_tree_commit(ctx, cur_k_layers, cur_v_layers, cur_len: torch.Tensor, path: torch.Tensor, n_path: torch.Tensor,
+                   new_len: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """cur_k_layers / cur_v_layers: one tensor [B, cur_cap, Hkv, d] per layer, changed in place; path int32 [B, max_path].
+    Returns new_len, int32 [B]."""
+    return (_native or _load_native()).tree_commit(ctx, _stream(stream), cur_k_layers, cur_v_layers, cur_len, path, n_path,
+                                                   new_len)
+
+
+# ---- eviction of single tokens ----------------------------------------------------------------------
+def ra_token_weights(ctx, q: torch.Tensor, view: KVView, lse: torch.Tensor, prev: Optional[torch.Tensor] = None,
+                     weights: Optional[torch.Tensor] = None, n_pos: Optional[int] = None,
+                     sel_idx: Optional[torch.Tensor] = None, n_sel: Optional[torch.Tensor] = None,
+                     scale: Optional[float] = None, stream=None) -> torch.Tensor:
+    """q [B, q_len, Hq, d] and lse [B, q_len, Hq], or q [B, Hq, d] and lse [B, Hq], as of the attention call; prev and weights
+    float32 [B, n_pos] (n_pos by default: prev's, then the view's max_tokens).  weights = prev updates in place."""
+    return (_native or _load_native()).token_weights(ctx, _stream(stream), q, view, lse, prev, weights, n_pos, sel_idx, n_sel,
+                                                     scale)
+
+
+def ra_select_tokens(ctx, weights: torch.Tensor, seg_len: torch.Tensor, n_rounds: torch.Tensor, budget: int,
+                     keep_first: int = 0, keep_last: int = 0, block_size: int = 0, stride: int = 0,
+                     kept_idx: Optional[torch.Tensor] = None, n_kept: Optional[torch.Tensor] = None,
+                     kept_len: Optional[torch.Tensor] = None, kept_off: Optional[torch.Tensor] = None,
+                     kept_weights: Optional[torch.Tensor] = None, stream=None
+                     ) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor, torch.Tensor, torch.Tensor]:
+    """Returns (kept_idx [B, budget], n_kept [B], kept_len [B, R_max], kept_off int64 [B, R_max], kept_weights [B, n_pos])."""
+    return (_native or _load_native()).select_tokens(ctx, _stream(stream), weights, seg_len, n_rounds, budget, keep_first,
+                                                     keep_last, block_size, stride, kept_idx, n_kept, kept_len, kept_off,
+                                                     kept_weights)
+
+
+def ra_compact_rounds(ctx, src: KVView, kept_idx: torch.Tensor, n_kept: torch.Tensor, dst: KVView, stream=None) -> None:
+    """Fills dst's keys and values with those of the kept tokens of src."""
+    (_native or _load_native()).compact_rounds(ctx, _stream(stream), src, kept_idx, n_kept, dst)
 
 
 # ---- round-indexed KV store ----------------------------------------------------------------------

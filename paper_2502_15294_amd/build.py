@@ -16,7 +16,7 @@ OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libround_attention.so")
 EXAMPLE_SRC = os.path.join(HERE, "examples", "decode_step.c")
 EXAMPLE = os.path.join(HERE, "ra_decode_step")  # plain C program driving the library through the C boundary alone
-SOURCES = ["context.hip", "decode.hip", "attn_mfma.hip", "attn_prefill_mfma.hip", "scores.hip", "scores_mfma.hip", "scores_prefill_mfma.hip", "select.hip", "prefill.hip", "kv_store.hip", "monitor.hip"]
+SOURCES = ["context.hip", "decode.hip", "attn_mfma.hip", "attn_prefill_mfma.hip", "scores.hip", "scores_mfma.hip", "scores_prefill_mfma.hip", "select.hip", "prefill.hip", "kv_store.hip", "monitor.hip", "tree.hip", "token_weights.hip", "evict.hip"]
 BINDING_SRC = os.path.join(CSRC, "binding.cpp")
 BINDING = os.path.join(HERE, "_binding.so")  # the compute calls' Python side (host code only)
 # packed-fp32 instruction selection is switched off for every device translation unit

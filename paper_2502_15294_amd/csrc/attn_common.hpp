@@ -67,7 +67,28 @@ struct AttnArgs {
     int max_parts;    // ... of which at most so many meet one sequence
     int grid;         // many-row kernel: workgroups
     int p_half;       // many-row kernel: probabilities as one fp16 operand instead of two bf16 (ra_set_prefill_precision)
+    // drafted tokens (q_len of them): which ones every one of them sees, and how many a sequence has (null: q_len).  The
+    // current round is then the cur_len_dev[b] committed tokens and, behind them, the drafted ones.
+    const uint32_t* tree_mask;  // [B][q_len][tree_words] or null
+    const int32_t* tree_len;    // [B] or null
+    int tree_words;
 };
+
+#ifdef __HIPCC__
+// Tokens of the current round that are committed, and drafted tokens behind them that it has rows for.
+__device__ __forceinline__ int committed_tokens(const AttnArgs& a, int b) { return min(max(a.cur_len_dev[b], 0), a.cur_cap); }
+__device__ __forceinline__ int drafted_tokens(const AttnArgs& a, int b, int committed) {
+    return min(a.tree_len ? min(max(a.tree_len[b], 0), a.q_len) : a.q_len, a.cur_cap - committed);
+}
+// Which of the 32 tokens from token `tok0` of the current round on a drafted token sees, bit by bit: the committed ones, and of
+// those behind them (drafted tokens tok0 - committed .. + 31) the ones in its row of the mask.
+__device__ __forceinline__ uint32_t tree_sees(const uint32_t* row, int words, int tok0, int committed) {
+    const int first = tok0 - committed, w = first >> 5, s = first & 31;
+    const uint32_t lo = w >= 0 && w < words ? row[w] : 0u, hi = w + 1 >= 0 && w + 1 < words ? row[w + 1] : 0u;
+    const uint32_t drafted = (uint32_t)(((unsigned long long)hi << 32 | lo) >> s);
+    return first >= 0 ? drafted : first <= -32 ? 0xffffffffu : drafted | ((1u << -first) - 1);
+}
+#endif
 
 // Workspace layout of one attention call; returns the bytes needed past the reserved head.
 struct AttnWorkspace {
@@ -110,6 +131,17 @@ inline size_t attn_mfma_inline_bytes(int B, int R_max) {
 inline bool attn_mfma_plans_inline(int B, int R_max) {
     return B <= kInlineBatch && (long long)B * R_max <= kInlineRounds;  // at most 29 KB of LDS beside the 17 KB of score staging
 }
+// Attention of several query tokens a sequence: a question, the question at the watershed layer (`scores` given), or a tree of
+// drafted tokens (`tree` given; cur_len is then the rows of cur_k).
+struct TreeOperands {
+    const int32_t* cur_len;
+    const uint32_t* mask;
+    const int32_t* len;
+};
+int question_attention(ra_ctx* ctx, const char* who, void* stream, const void* q, int q_len, int Hq, const ra_kv_view* layer,
+                       const int32_t* sel_idx, const int32_t* n_sel, const void* cur_k, const void* cur_v, int cur_len,
+                       float scale, float* out, float* lse, float* scores_head, float* scores, const TreeOperands* tree);
+
 // Launch shape and scratch of that kernel.  `max_tiles` bounds the 32-token key tiles of the whole batch.
 constexpr int kMfmaMinUnits = 4;     // shortest range in key tiles (two tiles are in flight per wave; ranges of 2 and of 8 measured no better)
 constexpr int kMfmaSpreadUnits = 2;  // ... and while the launch has waves to spare for all of them and the merge is quick (spread_longest)

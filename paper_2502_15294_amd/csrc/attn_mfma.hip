@@ -147,7 +147,8 @@ __global__ __launch_bounds__(256) void merge_records_kernel(AttnArgs a, int n_ro
 // layer; staged per wave in LDS and written out in runs of up to 64 tiles per row.
 // INLINE_PLAN: the workgroup resolves the batch's selections itself instead of reading the planning kernel's tables.
 // MAYBE_LONG (launches that plan inline): the ranges can be long enough for non-temporal value loads.
-template <int D, bool PAGED, bool TILE_LSE, bool INLINE_PLAN, bool MAYBE_LONG>
+// TREE: the query tokens are drafted ones, of which every one sees the committed tokens of the current round and its ancestors.
+template <int D, bool PAGED, bool TILE_LSE, bool INLINE_PLAN, bool MAYBE_LONG, bool TREE>
 __global__ __launch_bounds__(256, 2) void attn_mfma_kernel(AttnArgs a, int n_rowblocks) {
     constexpr int KK = D / 32, DT = D / 16, kParts = D == 64 ? 3 : 2;  // contraction steps of Q.K^T, 16-channel tiles of the output,
                                                                         // bf16 numbers a probability is carried as
@@ -210,6 +211,7 @@ __global__ __launch_bounds__(256, 2) void attn_mfma_kernel(AttnArgs a, int n_row
             c_rounds = vw.n_rounds[tid];
             if (a.sel_idx) c_sel = a.n_sel[tid];
             if (a.cur_k) c_cur = a.cur_len_dev ? a.cur_len_dev[tid] : a.cur_len_host;
+            if constexpr (TREE) c_cur = committed_tokens(a, tid), c_cur += drafted_tokens(a, tid, c_cur);
         }
         auto read_lists = [&](auto per_thread) {
             constexpr int N = decltype(per_thread)::value;
@@ -424,6 +426,12 @@ __global__ __launch_bounds__(256, 2) void attn_mfma_kernel(AttnArgs a, int n_row
                 for (int kk = 0; kk < KK; ++kk) qf[kk] = row_ok ? qp[kk * 4 + q4] : make_uint4(0, 0, 0, 0);
             }
 
+            int committed = 0, drafted = 0;
+            if constexpr (TREE) {
+                committed = uni(committed_tokens(a, b));
+                drafted = uni(drafted_tokens(a, b, committed));
+            }
+
             // ---- the sequence's segment table: a window of 64 entries in this wave's registers -------------
             int n_hist;  // segments before the current round's
             const char* plan_b = a.plan + (size_t)b * pstride;
@@ -590,7 +598,7 @@ __global__ __launch_bounds__(256, 2) void attn_mfma_kernel(AttnArgs a, int n_row
 
             auto consume = [&](KVTile<D>& t, const TileRef& r) {
                 const int tok0 = r.uin * kTile, len = r.len;
-                const bool full = !r.is_cur && (len - tok0 >= kTile);
+                const bool full = (!r.is_cur || (TREE && tok0 + kTile <= committed)) && (len - tok0 >= kTile);
                 floatx4_t sc[2];
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
@@ -604,13 +612,17 @@ __global__ __launch_bounds__(256, 2) void attn_mfma_kernel(AttnArgs a, int n_row
                         for (int dt = 0; dt < DT; ++dt) t.v[dt][1] = make_uint2(0, 0);
                     // tokens this row may see: the segment's length, or inside the current round the causal limit
                     int lim = len;
-                    if (r.is_cur) lim = min(len, max(len - q_len + qtok + 1, 0));
+                    if (r.is_cur && !TREE) lim = min(len, max(len - q_len + qtok + 1, 0));
                     if (!row_ok) lim = 0;
+                    uint32_t sees = 0xffffffffu;
+                    if (TREE && r.is_cur)
+                        sees = tree_sees(a.tree_mask + ((size_t)b * q_len + qtok) * a.tree_words, a.tree_words, tok0, committed);
 #pragma unroll
                     for (int h = 0; h < 2; ++h)
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
-                            if (tok0 + h * 16 + q4 * 4 + i >= lim) sc[h][i] = -__builtin_inff();
+                            if (tok0 + h * 16 + q4 * 4 + i >= lim || (TREE && !(sees >> (h * 16 + q4 * 4 + i) & 1)))
+                                sc[h][i] = -__builtin_inff();
                 }
                 float mx = fmaxf(fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[0][2], sc[0][3])),
                                  fmaxf(fmaxf(sc[1][0], sc[1][1]), fmaxf(sc[1][2], sc[1][3])));
@@ -721,6 +733,12 @@ __global__ __launch_bounds__(256, 2) void attn_mfma_kernel(AttnArgs a, int n_row
 
             // ---- the four lane groups hold partial sums of the same rows -------------------------------------
             l = xrow_sum4(l);
+            if (TREE && qtok >= drafted) {  // no token of this sequence's tree: as a row that sees nothing
+                m = kNegBig;
+                l = 0.f;
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt) acc[dt] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+            }
             if (whole) {
                 if (row_ok) {
                     const float inv = l > 0.f ? 1.f / l : 0.f;
@@ -755,15 +773,18 @@ static void launch_attn_mfma_d(const AttnArgs& a, bool paged, const MfmaDecodeSh
     const dim3 g((unsigned)s.grid), blk(256);
     const long long max_tiles = mfma_max_tiles(B, a.max_tokens, a.view.R_max, a.cur_cap);
     const bool maybe_long = inline_plan && max_tiles > (kMfmaMinUnits + 1ll) * s.max_ranges;
-#define RA_ATTN_CASE(P_, L_, I_, M_)                                                                      \
-    if (paged == P_ && tile_lse == L_ && inline_plan == I_ && maybe_long == M_) {                         \
-        RA_LAUNCH_TIMED((attn_mfma_kernel<D, P_, L_, I_, M_>), g, blk, smem, st, a, s.n_rowblocks);       \
+    const bool tree = a.tree_mask != nullptr;  // (without scores)
+#define RA_ATTN_CASE(P_, L_, I_, M_, T_)                                                                  \
+    if (paged == P_ && tile_lse == L_ && inline_plan == I_ && maybe_long == M_ && tree == T_) {           \
+        RA_LAUNCH_TIMED((attn_mfma_kernel<D, P_, L_, I_, M_, T_>), g, blk, smem, st, a, s.n_rowblocks);   \
         return;                                                                                           \
     }
-#define RA_ATTN_CASES(P_, L_) RA_ATTN_CASE(P_, L_, false, false) RA_ATTN_CASE(P_, L_, true, false) RA_ATTN_CASE(P_, L_, true, true)
-    RA_ATTN_CASES(false, false) RA_ATTN_CASES(true, false)
+#define RA_ATTN_CASES(P_, L_, T_) \
+    RA_ATTN_CASE(P_, L_, false, false, T_) RA_ATTN_CASE(P_, L_, true, false, T_) RA_ATTN_CASE(P_, L_, true, true, T_)
+    RA_ATTN_CASES(false, false, false) RA_ATTN_CASES(true, false, false)
+    RA_ATTN_CASES(false, false, true) RA_ATTN_CASES(true, false, true)
     if constexpr (D == 128) {  // scores from the attention pass: 128 channels only
-        RA_ATTN_CASES(false, true) RA_ATTN_CASES(true, true)
+        RA_ATTN_CASES(false, true, false) RA_ATTN_CASES(true, true, false)
     }
 #undef RA_ATTN_CASES
 #undef RA_ATTN_CASE

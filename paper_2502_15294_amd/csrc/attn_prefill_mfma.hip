@@ -77,7 +77,8 @@ struct Share {
 // RAGGED: some wave of some row block has fewer than two row tiles.  (A variant of its own: with the choice of tile counts in
 // its loop the kernel takes 412 instead of 400 microseconds for the 512 rows of a 128-token question at the watershed
 // layer, which need none, paged 502 instead of 483; without the scores 147 and 145.)
-template <bool PAGED, bool TILE_LSE, bool P_HALF, bool INLINE_PLAN, bool RAGGED>
+// TREE: the query tokens are drafted ones, of which every one sees the committed tokens of the current round and its ancestors.
+template <bool PAGED, bool TILE_LSE, bool P_HALF, bool INLINE_PLAN, bool RAGGED, bool TREE>
 __global__ __launch_bounds__(256, kWorkgroupsPerCuP) void attn_prefill_mfma_kernel(AttnArgs a, int n_rowblocks) {
     extern __shared__ __align__(16) char smem[];
     __shared__ int sU[INLINE_PLAN ? kInlineBatch : kMaxBatch], sps[INLINE_PLAN ? 1 : kMaxBatch + 1];
@@ -101,7 +102,11 @@ __global__ __launch_bounds__(256, kWorkgroupsPerCuP) void attn_prefill_mfma_kern
     int P;
     BatchLists lists;
     if constexpr (INLINE_PLAN) {
-        lists.load(tiles + 2 * kTileBytes, vw, a.sel_idx, a.n_sel, [&](int) { return a.cur_k ? a.cur_len_host : 0; });
+        int my_cur = 0;  // thread b: the current round of sequence b
+        if constexpr (TREE) {
+            if (tid < vw.B) my_cur = committed_tokens(a, tid), my_cur += drafted_tokens(a, tid, my_cur);
+        }
+        lists.load(tiles + 2 * kTileBytes, vw, a.sel_idx, a.n_sel, [&](int) { return TREE ? my_cur : a.cur_k ? a.cur_len_host : 0; });
         lists.count_tiles(vw.B, sU);
         P = cut_tiles<kWorkgroupsPerCuP>(ranges, sU, vw.B, a.slots, a.min_units, a.max_parts,
                                          !PAGED && !P_HALF && gridDim.x >= kWorkgroupsPerCuP * (unsigned)a.num_cu &&
@@ -196,6 +201,11 @@ __global__ __launch_bounds__(256, kWorkgroupsPerCuP) void attn_prefill_mfma_kern
             const uint4* qp = reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(a.q) + rowid[nt] * 256);
 #pragma unroll
             for (int kk = 0; kk < 4; ++kk) qf[nt][kk] = qp[kk * 4 + q4];  // rows past the last repeat row 0, unused
+        }
+        int committed = 0, drafted = 0;
+        if constexpr (TREE) {
+            committed = uniform(committed_tokens(a, b));
+            drafted = uniform(drafted_tokens(a, b, committed));
         }
         int n_slots, n_hist;
         if (!INLINE_PLAN || !first) __syncthreads();  // the previous pass's readers of the table and the tile buffers are done
@@ -362,7 +372,7 @@ __global__ __launch_bounds__(256, kWorkgroupsPerCuP) void attn_prefill_mfma_kern
         // N: row tiles of this wave (1 or 2)
         auto consume = [&](auto n_tiles, const char* buf, int tok0, int len, bool is_cur) {
             constexpr int N = decltype(n_tiles)::value;
-            const bool full = !is_cur && (len - tok0 >= kTileP);
+            const bool full = (!is_cur || (TREE && tok0 + kTileP <= committed)) && (len - tok0 >= kTileP);
             const uint4* kb = reinterpret_cast<const uint4*>(buf);
             const uint4* vb = reinterpret_cast<const uint4*>(buf + 8192);
             uint4 kf[2][4];
@@ -383,13 +393,17 @@ __global__ __launch_bounds__(256, kWorkgroupsPerCuP) void attn_prefill_mfma_kern
                 for (int nt = 0; nt < N; ++nt) {
                     // tokens this row may see: the segment's length, or inside the current round the causal limit
                     int lim = len;
-                    if (is_cur) lim = min(len, max(len - q_len + qtok[nt] + 1, 0));
+                    if (is_cur && !TREE) lim = min(len, max(len - q_len + qtok[nt] + 1, 0));
                     if (!row_ok[nt]) lim = 0;
+                    uint32_t sees = 0xffffffffu;
+                    if (TREE && is_cur)
+                        sees = tree_sees(a.tree_mask + ((size_t)b * q_len + qtok[nt]) * a.tree_words, a.tree_words, tok0, committed);
 #pragma unroll
                     for (int h = 0; h < 2; ++h)
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
-                            if (tok0 + q4 * 8 + h * 4 + i >= lim) sc[nt][h][i] = -__builtin_inff();
+                            if (tok0 + q4 * 8 + h * 4 + i >= lim || (TREE && !(sees >> (q4 * 8 + h * 4 + i) & 1)))
+                                sc[nt][h][i] = -__builtin_inff();
                 }
             }
             // The reference logit m of a row is only raised when some logit exceeds it by more than `slack`
@@ -531,6 +545,12 @@ __global__ __launch_bounds__(256, kWorkgroupsPerCuP) void attn_prefill_mfma_kern
 #pragma unroll
                 for (int dt = 0; dt < 8; ++dt) acc[nt][dt] *= unscale;
             }
+            if (TREE && qtok[nt] >= drafted) {  // no token of this sequence's tree: as a row that sees nothing
+                m[nt] = kNegBig;
+                l[nt] = 0.f;
+#pragma unroll
+                for (int dt = 0; dt < 8; ++dt) acc[nt][dt] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+            }
             if (!row_ok[nt]) continue;
             if (!whole) {
                 const size_t pr = rowid[nt] * a.S + s;
@@ -586,17 +606,20 @@ int launch_attn_prefill_mfma(const AttnArgs& a, bool paged, hipStream_t st) {
     const bool lse = a.tile_lse != nullptr, half = a.p_half != 0;
     const int row_tiles = (rows_total + 15) / 16;
     const bool ragged = row_tiles != n_rowblocks * 4 * kNTP;
-#define RA_PREFILL_CASE(P_, L_, H_, I_, R_)                                                                          \
-    if (paged == P_ && lse == L_ && half == H_ && plan_inline == I_ && ragged == R_) {                               \
-        RA_LAUNCH_TIMED((attn_prefill_mfma_kernel<P_, L_, H_, I_, R_>), dim3((unsigned)grid), dim3(256), smem, st, a, n_rowblocks); \
+    const bool tree = a.tree_mask != nullptr;  // (with neither scores nor the fp16 mode)
+#define RA_PREFILL_CASE(P_, L_, H_, I_, R_, T_)                                                                      \
+    if (paged == P_ && lse == L_ && half == H_ && plan_inline == I_ && ragged == R_ && tree == T_) {                 \
+        RA_LAUNCH_TIMED((attn_prefill_mfma_kernel<P_, L_, H_, I_, R_, T_>), dim3((unsigned)grid), dim3(256), smem, st, a, n_rowblocks); \
         return RA_OK;                                                                                                \
     }
-#define RA_PREFILL_CASES(L_, H_, R_)                                                                                 \
-    RA_PREFILL_CASE(false, L_, H_, false, R_) RA_PREFILL_CASE(true, L_, H_, false, R_)                               \
-    RA_PREFILL_CASE(false, L_, H_, true, R_) RA_PREFILL_CASE(true, L_, H_, true, R_)
-    RA_PREFILL_CASES(false, false, false) RA_PREFILL_CASES(true, false, false) RA_PREFILL_CASES(false, true, false)
-    RA_PREFILL_CASES(true, true, false) RA_PREFILL_CASES(false, false, true) RA_PREFILL_CASES(true, false, true)
-    RA_PREFILL_CASES(false, true, true) RA_PREFILL_CASES(true, true, true)
+#define RA_PREFILL_CASES(L_, H_, R_, T_)                                                                             \
+    RA_PREFILL_CASE(false, L_, H_, false, R_, T_) RA_PREFILL_CASE(true, L_, H_, false, R_, T_)                       \
+    RA_PREFILL_CASE(false, L_, H_, true, R_, T_) RA_PREFILL_CASE(true, L_, H_, true, R_, T_)
+    RA_PREFILL_CASES(false, false, false, false) RA_PREFILL_CASES(true, false, false, false)
+    RA_PREFILL_CASES(false, true, false, false) RA_PREFILL_CASES(true, true, false, false)
+    RA_PREFILL_CASES(false, false, true, false) RA_PREFILL_CASES(true, false, true, false)
+    RA_PREFILL_CASES(false, true, true, false) RA_PREFILL_CASES(true, true, true, false)
+    RA_PREFILL_CASES(false, false, false, true) RA_PREFILL_CASES(false, false, true, true)
 #undef RA_PREFILL_CASES
 #undef RA_PREFILL_CASE
     return RA_OK;

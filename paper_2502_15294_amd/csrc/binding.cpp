@@ -14,6 +14,8 @@
 #include <ATen/ATen.h>
 #include <cmath>
 #include <cstring>
+#include <string>
+#include <vector>
 
 #include "round_attention.h"
 
@@ -28,6 +30,11 @@ struct Functions {
     decltype(&ra_watershed_attn_decode) watershed_decode;
     decltype(&ra_round_sparse_attn_prefill) prefill;
     decltype(&ra_watershed_attn_prefill) watershed_prefill;
+    decltype(&ra_round_sparse_attn_tree) tree;
+    decltype(&ra_tree_commit) tree_commit;
+    decltype(&ra_token_weights) token_weights;
+    decltype(&ra_select_tokens) select_tokens;
+    decltype(&ra_compact_rounds) compact_rounds;
 } fn;
 PyObject* on_error = nullptr;  // called with a status that is not RA_OK; raises
 PyObject* name_c = nullptr;    // "c"
@@ -120,6 +127,36 @@ void want_dims(const at::Tensor& t, int64_t dims) {
     PyErr_Format(PyExc_ValueError, "a tensor of %d dimensions is needed here, this one has %d", (int)dims, (int)t.dim());
     throw PythonError();
 }
+// A tensor of the calls on drafted tokens and on single tokens: of this type and these sizes (-1: any), on the device of `like`.
+const at::Tensor* expect(const char* name, PyObject* o, at::ScalarType type, at::IntArrayRef sizes, const at::Tensor& like) {
+    const at::Tensor* t = tensor_or_null(o);
+    if (!t) return nullptr;
+    bool fits = t->scalar_type() == type && t->dim() == (int64_t)sizes.size() && t->device() == like.device();
+    for (size_t i = 0; fits && i < sizes.size(); ++i) fits = sizes[i] < 0 || t->size((int64_t)i) == sizes[i];
+    if (fits) return t;
+    std::string want;
+    for (const int64_t n : sizes) want += (want.empty() ? "" : ", ") + (n < 0 ? std::string("*") : std::to_string(n));
+    PyErr_Format(PyExc_ValueError, "%s: a %s tensor of sizes [%s] on the inputs' device is needed", name, c10::toString(type), want.c_str());
+    throw PythonError();
+}
+template <typename T>
+T* expected(const char* name, PyObject* o, at::IntArrayRef sizes, const at::Tensor& like) {
+    const at::Tensor* t = expect(name, o, c10::CppTypeToScalarType<T>::value, sizes, like);
+    return t ? static_cast<T*>(data(*t)) : nullptr;
+}
+at::ScalarType type_of(const View& view) { return view->dtype == RA_BF16 ? at::kBFloat16 : at::kFloat; }
+long long integer(PyObject* o) {
+    const long long v = PyLong_AsLongLong(o);
+    if (v == -1 && PyErr_Occurred()) throw PythonError();
+    return v;
+}
+int integer32(const char* name, PyObject* o) {
+    const long long v = integer(o);
+    if (v == (int)v) return (int)v;
+    PyErr_Format(PyExc_OverflowError, "%s does not fit 32 bits", name);
+    throw PythonError();
+}
+
 int second_size(PyObject* o) {  // tokens of the current round; 0 without one
     const at::Tensor* t = tensor_or_null(o);
     return t ? (int)t->size(1) : 0;
@@ -351,6 +388,160 @@ PyObject* watershed_prefill(PyObject* const* a) {
         out, lse, ph, p);
 }
 
+// (ctx, stream, q, view, tree_mask, cur_k, cur_v, cur_len, tree_len, sel_idx, n_sel, scale, out, lse)
+PyObject* tree(PyObject* const* a) {
+    const at::Tensor& q = tensor(a[2]);
+    want_dims(q, 4);
+    const View view(a[3]);
+    const int64_t B = view->B, n = q.size(1), Hq = q.size(2), d = view->d, R = view->R_max;
+    expect("q", a[2], type_of(view), {B, n, Hq, d}, q);
+    const at::Tensor* ck_tensor = expect("cur_k", a[5], type_of(view), {B, -1, view->Hkv, d}, q);
+    const int64_t cap = ck_tensor ? ck_tensor->size(1) : 0;
+    expect("cur_v", a[6], type_of(view), {B, cap, view->Hkv, d}, q);
+    const uint32_t* mask = reinterpret_cast<uint32_t*>(expected<int32_t>("tree_mask", a[4], {B, n, (n + 31) / 32}, q));
+    const int32_t *cl = expected<int32_t>("cur_len", a[7], {B}, q), *tl = expected<int32_t>("tree_len", a[8], {B}, q);
+    const int32_t *sel = expected<int32_t>("sel_idx", a[9], {B, R}, q), *ns = expected<int32_t>("n_sel", a[10], {B}, q);
+    expected<float>("out", a[12], {B, n, Hq, d}, q);
+    expected<float>("lse", a[13], {B, n, Hq}, q);
+    Output<float> out(a[12], {B, n, Hq, d}, q), lse(a[13], {B, n, Hq}, q);
+    ra_ctx* ctx = context(a[0]);
+    void *st = handle(a[1]), *qp = data(q), *ck = data(a[5]), *cv = data(a[6]);
+    const float scale = scale_of(a[11], d);
+    return checked(
+        [&] { return fn.tree(ctx, st, qp, (int)n, (int)Hq, view.p, sel, ns, ck, cv, cl, (int)cap, mask, tl, scale, out.p, lse.p); },
+        out, lse);
+}
+
+// The tensors of a list or tuple: one per layer, all of the first one's type, sizes and device.
+struct Layers {
+    std::vector<void*> p;
+    const at::Tensor* first = nullptr;
+    Layers(const char* name, PyObject* o, const at::Tensor* like) {
+        PyObject* items = PySequence_Fast(o, "a list of tensors, one per layer, is needed");
+        if (!items) throw PythonError();
+        const Py_ssize_t n = PySequence_Fast_GET_SIZE(items);
+        try {
+            for (Py_ssize_t i = 0; i < n; ++i) {
+                PyObject* item = PySequence_Fast_GET_ITEM(items, i);
+                const at::Tensor& t = tensor(item);
+                if (!first) first = like ? like : &t;
+                p.push_back(data(*expect(name, item, first->scalar_type(), first->sizes(), *first)));
+            }
+        } catch (...) {
+            Py_DECREF(items);
+            throw;
+        }
+        Py_DECREF(items);  // (the caller's list keeps the tensors)
+    }
+};
+
+// (ctx, stream, cur_k_layers, cur_v_layers, cur_len, path, n_path, new_len)
+PyObject* tree_commit(PyObject* const* a) {
+    const Layers k("cur_k_layers", a[2], nullptr);
+    const Layers v("cur_v_layers", a[3], k.first);
+    if (!k.first || k.p.size() != v.p.size()) {
+        PyErr_SetString(PyExc_ValueError, "as many keys as values, and one layer at least, are needed");
+        throw PythonError();
+    }
+    const at::Tensor& like = *k.first;
+    want_dims(like, 4);
+    if (like.scalar_type() != at::kBFloat16 && like.scalar_type() != at::kFloat) {
+        PyErr_Format(PyExc_TypeError, "unsupported KV dtype %s", c10::toString(like.scalar_type()));
+        throw PythonError();
+    }
+    const int64_t B = like.size(0);
+    const at::Tensor* path_tensor = expect("path", a[5], at::kInt, {B, -1}, like);
+    const int32_t *cl = expected<int32_t>("cur_len", a[4], {B}, like), *path = data<int32_t>(a[5]);
+    const int32_t* np = expected<int32_t>("n_path", a[6], {B}, like);
+    expected<int32_t>("new_len", a[7], {B}, like);
+    Output<int32_t> new_len(a[7], {B}, like);
+    ra_ctx* ctx = context(a[0]);
+    void* st = handle(a[1]);
+    return checked(
+        [&] { return fn.tree_commit(ctx, st, k.p.data(), v.p.data(), (int)k.p.size(), (int)B, (int)like.size(1), (int)like.size(2),
+                                    (int)like.size(3), like.scalar_type() == at::kBFloat16 ? RA_BF16 : RA_F32, cl, path, np,
+                                    path_tensor ? (int)path_tensor->size(1) : 0, new_len.p); },
+        new_len);
+}
+
+// (ctx, stream, q, view, lse, prev, weights, n_pos, sel_idx, n_sel, scale)
+PyObject* token_weights(PyObject* const* a) {
+    const at::Tensor& q = tensor(a[2]);
+    if (q.dim() != 3) want_dims(q, 4);
+    const View view(a[3]);
+    const bool one = q.dim() == 3;  // the form of the decode call: one query token
+    const int64_t B = view->B, q_len = one ? 1 : q.size(1), Hq = q.size(one ? 1 : 2), d = view->d, R = view->R_max;
+    expect("q", a[2], type_of(view), one ? at::DimVector{B, Hq, d} : at::DimVector{B, q_len, Hq, d}, q);
+    const float* lse = expected<float>("lse", a[4], one ? at::DimVector{B, Hq} : at::DimVector{B, q_len, Hq}, q);
+    const at::Tensor *prev_tensor = expect("prev", a[5], at::kFloat, {B, -1}, q), *weights_tensor = expect("weights", a[6], at::kFloat, {B, -1}, q);
+    const int64_t n_pos = weights_tensor ? weights_tensor->size(1) : a[7] != Py_None ? integer(a[7]) : prev_tensor ? prev_tensor->size(1) : view->max_tokens;
+    const float* prev = expected<float>("prev", a[5], {B, n_pos}, q);
+    if (n_pos < 0 || n_pos != (int)n_pos) {
+        PyErr_SetString(PyExc_ValueError, "n_pos must be a positive number of 32 bits");
+        throw PythonError();
+    }
+    Output<float> weights(a[6], {B, n_pos}, q);
+    const int32_t *sel = expected<int32_t>("sel_idx", a[8], {B, R}, q), *ns = expected<int32_t>("n_sel", a[9], {B}, q);
+    ra_ctx* ctx = context(a[0]);
+    void *st = handle(a[1]), *qp = data(q);
+    const float scale = scale_of(a[10], d);
+    return checked(
+        [&] { return fn.token_weights(ctx, st, qp, (int)q_len, (int)Hq, view.p, sel, ns, lse, scale, prev, weights.p, (int)n_pos); },
+        weights);
+}
+
+// (ctx, stream, weights, seg_len, n_rounds, budget, keep_first, keep_last, block_size, stride, kept_idx, n_kept, kept_len,
+//  kept_off, kept_weights)
+PyObject* select_tokens(PyObject* const* a) {
+    const at::Tensor& w = tensor(a[2]);
+    want_dims(w, 2);
+    const int64_t B = w.size(0), n_pos = w.size(1);
+    expect("weights", a[2], at::kFloat, {B, n_pos}, w);
+    const at::Tensor* lens = expect("seg_len", a[3], at::kInt, {B, -1}, w);
+    const int64_t R = lens ? lens->size(1) : 0;
+    const int32_t *len = data<int32_t>(a[3]), *n = expected<int32_t>("n_rounds", a[4], {B}, w);
+    ra_keep_params params = {integer32("budget", a[5]), integer32("keep_first", a[6]), integer32("keep_last", a[7]),
+                             integer32("block_size", a[8]), integer(a[9])};
+    const int64_t budget = params.budget > 0 ? params.budget : 0;
+    expected<int32_t>("kept_idx", a[10], {B, budget}, w);
+    expected<int32_t>("n_kept", a[11], {B}, w);
+    expected<int32_t>("kept_len", a[12], {B, R}, w);
+    expected<int64_t>("kept_off", a[13], {B, R}, w);
+    expected<float>("kept_weights", a[14], {B, n_pos}, w);
+    Output<int32_t> idx(a[10], {B, budget}, w), count(a[11], {B}, w), kept_len(a[12], {B, R}, w);
+    Output<int64_t> off(a[13], {B, R}, w);
+    Output<float> left(a[14], {B, n_pos}, w);
+    ra_ctx* ctx = context(a[0]);
+    void* st = handle(a[1]);
+    const float* wp = static_cast<float*>(data(w));
+    if (n_pos != (int)n_pos) {
+        PyErr_SetString(PyExc_ValueError, "weights has too many columns");
+        throw PythonError();
+    }
+    return checked(
+        [&] { return fn.select_tokens(ctx, st, wp, (int)n_pos, len, n, (int)B, (int)R, &params, idx.p, count.p, kept_len.p, off.p,
+                                      left.p); },
+        idx, count, kept_len, off, left);
+}
+
+// (ctx, stream, src, kept_idx, n_kept, dst)
+PyObject* compact_rounds(PyObject* const* a) {
+    const View src(a[2]), dst(a[5]);
+    const at::Tensor& idx = tensor(a[3]);
+    want_dims(idx, 2);
+    const int64_t B = src->B, K = idx.size(1);
+    const int32_t *ip = expected<int32_t>("kept_idx", a[3], {B, K}, idx), *n = expected<int32_t>("n_kept", a[4], {B}, idx);
+    ra_ctx* ctx = context(a[0]);
+    void* st = handle(a[1]);
+    int rc;
+    {
+        const Released released;
+        rc = fn.compact_rounds(ctx, st, src.p, ip, n, (int)K, dst.p);
+    }
+    if (rc != RA_OK) return PyObject_CallFunction(on_error, "i", rc);
+    Py_RETURN_NONE;
+}
+
 // The Python function: argument count, C++ exceptions (an allocation that fails among them) turned into Python's.
 template <PyObject* (*F)(PyObject* const*), Py_ssize_t N>
 PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
@@ -410,6 +601,11 @@ PyMethodDef methods[] = {
     RA_METHOD(watershed_decode, 12),
     RA_METHOD(prefill, 11),
     RA_METHOD(watershed_prefill, 11),
+    RA_METHOD(tree, 14),
+    RA_METHOD(tree_commit, 8),
+    RA_METHOD(token_weights, 11),
+    RA_METHOD(select_tokens, 15),
+    RA_METHOD(compact_rounds, 6),
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

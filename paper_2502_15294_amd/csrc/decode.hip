@@ -45,6 +45,7 @@ __global__ __launch_bounds__(256) void plan_kernel(AttnArgs a, int unit_tokens) 
     const int n_hist = a.sel_idx ? min(max(a.n_sel[b], 0), vw.R_max) : n_rounds;
     int cur_len = 0;
     if (a.cur_k) cur_len = min(max(a.cur_len_dev ? a.cur_len_dev[b] : a.cur_len_host, 0), a.cur_cap);
+    if (a.tree_mask) cur_len += drafted_tokens(a, b, cur_len);
     const int n_slots = n_hist + (cur_len > 0 ? 1 : 0);
     for (int i = tid; i < cap; i += 256) {
         int len = 0;

@@ -9,37 +9,38 @@
 
 using namespace ra;
 
-// Shared by the two prefill entry points.  With `scores` given (watershed layer) the attention runs over every
+// Shared by the two prefill entry points and the tree's.  With `scores` given (watershed layer) the attention runs over every
 // history round and the kernel also leaves one log-sum-exp per (query row, score unit: a 32-token key tile in the
 // 16-row kernel, what a piece has of a round in the many-row kernel), which the finishing kernels of the score
 // pass turn into Eq. 1.
-static int prefill_impl(ra_ctx* ctx, void* stream, const void* q, int q_len, int Hq, const ra_kv_view* layer,
-                        const int32_t* sel_idx, const int32_t* n_sel, const void* cur_k, const void* cur_v, int cur_len,
-                        float scale, float* out, float* lse, float* scores_head, float* scores) {
-    RA_REQUIRE(ctx != nullptr, RA_ERR_INVALID_ARG, "prefill: ctx is NULL");
-    RA_REQUIRE(q != nullptr && out != nullptr, RA_ERR_INVALID_ARG, "prefill: q or out is NULL");
-    if (int rc = check_view(layer, true, "prefill")) return rc;
-    RA_REQUIRE(q_len > 0, RA_ERR_INVALID_ARG, "prefill: q_len must be positive");
-    RA_REQUIRE(Hq > 0 && Hq % layer->Hkv == 0, RA_ERR_INVALID_ARG, "prefill: Hq %d is not a multiple of Hkv %d", Hq,
+int ra::question_attention(ra_ctx* ctx, const char* who, void* stream, const void* q, int q_len, int Hq, const ra_kv_view* layer,
+                           const int32_t* sel_idx, const int32_t* n_sel, const void* cur_k, const void* cur_v, int cur_len,
+                           float scale, float* out, float* lse, float* scores_head, float* scores, const TreeOperands* tree) {
+    RA_REQUIRE(ctx != nullptr, RA_ERR_INVALID_ARG, "%s: ctx is NULL", who);
+    RA_REQUIRE(q != nullptr && out != nullptr, RA_ERR_INVALID_ARG, "%s: q or out is NULL", who);
+    if (int rc = check_view(layer, true, who)) return rc;
+    RA_REQUIRE(q_len > 0, RA_ERR_INVALID_ARG, "%s: q_len must be positive", who);
+    RA_REQUIRE(Hq > 0 && Hq % layer->Hkv == 0, RA_ERR_INVALID_ARG, "%s: Hq %d is not a multiple of Hkv %d", who, Hq,
                layer->Hkv);
     RA_REQUIRE((sel_idx == nullptr) == (n_sel == nullptr), RA_ERR_INVALID_ARG,
-               "prefill: sel_idx and n_sel must both be given or both be NULL");
+               "%s: sel_idx and n_sel must both be given or both be NULL", who);
     RA_REQUIRE(cur_len >= 0 && (cur_k != nullptr) == (cur_len > 0) && (cur_v != nullptr) == (cur_len > 0),
-               RA_ERR_INVALID_ARG, "prefill: cur_k, cur_v and cur_len > 0 must be given together");
+               RA_ERR_INVALID_ARG, "%s: cur_k, cur_v and cur_len > 0 must be given together", who);
     RA_REQUIRE(cur_len == 0 || cur_len >= q_len, RA_ERR_INVALID_ARG,
-               "prefill: the q_len query tokens are the tail of the current round, so cur_len >= q_len");
+               "%s: the q_len query tokens are the tail of the current round, so cur_len >= q_len", who);
     RA_REQUIRE(layer->R_max > 0 || cur_len > 0, RA_ERR_INVALID_ARG,
-               "prefill: no history rounds and no current round: the key set is empty");
-    RA_REQUIRE(scale > 0.f && scale == scale, RA_ERR_INVALID_ARG, "prefill: scale must be positive");
-    RA_REQUIRE(layer->dtype == RA_BF16 && layer->d == 128, RA_ERR_UNSUPPORTED,
-               "prefill: only bf16 with head_dim 128 is implemented");
-    const int G = Hq / layer->Hkv, B = layer->B, D = 128;
-    RA_REQUIRE(G <= 16, RA_ERR_UNSUPPORTED, "prefill: Hq / Hkv = %d exceeds 16", G);
-    RA_REQUIRE(B <= kMaxBatch, RA_ERR_UNSUPPORTED, "prefill: batch %d exceeds %d", B, kMaxBatch);
+               "%s: no history rounds and no current round: the key set is empty", who);
+    RA_REQUIRE(scale > 0.f && scale == scale, RA_ERR_INVALID_ARG, "%s: scale must be positive", who);
+    RA_REQUIRE(layer->dtype == RA_BF16 && (layer->d == 128 || (tree && layer->d == 64)), RA_ERR_UNSUPPORTED,
+               "%s: only bf16 with head_dim 128 is implemented", who);
+    const int G = Hq / layer->Hkv, B = layer->B, D = layer->d;
+    RA_REQUIRE(G <= 16, RA_ERR_UNSUPPORTED, "%s: Hq / Hkv = %d exceeds 16", who, G);
+    RA_REQUIRE(B <= kMaxBatch, RA_ERR_UNSUPPORTED, "%s: batch %d exceeds %d", who, B, kMaxBatch);
 
     // Few query rows per KV head: the decode kernel (one wave per range of key tiles and block of 16 rows);
     // otherwise the kernel whose waves own different rows and share each key tile through LDS.
-    const bool few_rows = q_len * G <= 32;
+    // (Heads of 64 channels: always the decode kernel, whose blocks of rows each read the keys.)
+    const bool few_rows = q_len * G <= 32 || D == 64;
     const size_t rows = (size_t)B * q_len * Hq;
     const bool with_scores = scores != nullptr;
     RA_REQUIRE(!with_scores || layer->R_max > 0, RA_ERR_INVALID_ARG, "watershed prefill: R_max is 0, there is nothing to score");
@@ -65,6 +66,7 @@ static int prefill_impl(ra_ctx* ctx, void* stream, const void* q, int q_len, int
     a.S = 1;
     a.min_units = few_rows ? kMfmaMinUnits : attn_min_units();
     a.num_cu = ctx->num_cu;
+    int num_cu = ctx->num_cu;
     MfmaDecodeShape shape = {};
     MfmaDecodeWorkspace mw = {};
     AttnWorkspace w = {};
@@ -72,9 +74,12 @@ static int prefill_impl(ra_ctx* ctx, void* stream, const void* q, int q_len, int
     size_t plan_off, scratch_total;
     if (few_rows) {
         const long long max_tiles = mfma_max_tiles(B, layer->max_tokens, layer->R_max, cur_len);
-        RA_REQUIRE(max_tiles < ((long long)1 << 30), RA_ERR_UNSUPPORTED, "prefill: max_tokens too large for this batch");
-        a.shape_units = mfma_decode_fit(ctx->num_cu, B, layer->R_max, layer->Hkv, D, q_len * G, max_tiles,
-                                        ctx->ws.bytes > score_bytes ? ctx->ws.bytes - score_bytes : 0, shape, mw);
+        RA_REQUIRE(max_tiles < ((long long)1 << 30), RA_ERR_UNSUPPORTED, "%s: max_tokens too large for this batch", who);
+        for (;; num_cu /= 2) {  // (many blocks of rows: as large a launch as the workspace has room for)
+            a.shape_units = mfma_decode_fit(num_cu, B, layer->R_max, layer->Hkv, D, q_len * G, max_tiles,
+                                            ctx->ws.bytes > score_bytes ? ctx->ws.bytes - score_bytes : 0, shape, mw);
+            if (D == 128 || mw.total + score_bytes <= ctx->ws.bytes || num_cu < 2) break;
+        }
         plan_off = mw.plan_off;
         scratch_total = mw.total;
     } else {
@@ -95,7 +100,7 @@ static int prefill_impl(ra_ctx* ctx, void* stream, const void* q, int q_len, int
         int S = mfma_max_pieces(layer->max_tokens + cur_len, a.min_units, 8);
         const size_t least = attn_workspace(rows, S, D, B, layer->R_max).total + score_bytes;
         RA_REQUIRE(ctx->ws.base != nullptr && ctx->ws.bytes >= least, RA_ERR_WORKSPACE,
-                   "prefill: workspace has %zu bytes, this call needs %zu", ctx->ws.bytes, least);
+                   "%s: workspace has %zu bytes, this call needs %zu", who, ctx->ws.bytes, least);
         const int of_eight = mfma_max_pieces(layer->max_tokens + cur_len, a.min_units, 16) + 2;
         for (int units : {kPrefillMinUnits, a.min_units}) {
             if (plan_inline) break;
@@ -121,7 +126,7 @@ static int prefill_impl(ra_ctx* ctx, void* stream, const void* q, int q_len, int
         scratch_total = w.total;
     }
     RA_REQUIRE(ctx->ws.base != nullptr && ctx->ws.bytes >= scratch_total + score_bytes, RA_ERR_WORKSPACE,
-               "prefill: workspace has %zu bytes, this call needs %zu", ctx->ws.bytes, scratch_total + score_bytes);
+               "%s: workspace has %zu bytes, this call needs %zu", who, ctx->ws.bytes, scratch_total + score_bytes);
 
     a.q = q;
     a.sel_idx = sel_idx;
@@ -129,6 +134,12 @@ static int prefill_impl(ra_ctx* ctx, void* stream, const void* q, int q_len, int
     a.cur_k = cur_len ? cur_k : nullptr;
     a.cur_v = cur_len ? cur_v : nullptr;
     a.cur_len_dev = nullptr;
+    if (tree) {
+        a.cur_len_dev = tree->cur_len;
+        a.tree_mask = tree->mask;
+        a.tree_len = tree->len;
+        a.tree_words = (q_len + 31) / 32;
+    }
     a.c = scale * kLog2e;
     a.scale = scale;
     a.part_acc = few_rows ? nullptr : reinterpret_cast<float*>(ctx->ws.base + w.acc_off);
@@ -146,17 +157,17 @@ static int prefill_impl(ra_ctx* ctx, void* stream, const void* q, int q_len, int
     a.rec_ml = few_rows ? reinterpret_cast<float*>(ctx->ws.base + mw.ml_off) : nullptr;
     a.seq_rec = reinterpret_cast<int*>(ctx->ws.base + kWsSeqRecOff);
     a.max_ranges = shape.max_ranges;
-    a.p_half = with_scores ? 0 : ctx->prefill_p_half;  // the watershed call's scores decide the selection: full precision
+    a.p_half = with_scores || tree ? 0 : ctx->prefill_p_half;  // the watershed call's scores decide the selection: full precision
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
     a.plan_inline = plan_inline;
     if (!plan_inline) launch_plan(a, 32, st);
     {
         KernelTimer timer(ctx, st);
-        if (int rc = few_rows ? launch_attn_mfma(a, layer->block_size != 0, ctx->num_cu, st)
+        if (int rc = few_rows ? launch_attn_mfma(a, layer->block_size != 0, num_cu, st)
                               : launch_attn_prefill_mfma(a, layer->block_size != 0, st))
             return rc;
     }
-    if (few_rows) launch_merge_records(a, ctx->num_cu, st);
+    if (few_rows) launch_merge_records(a, num_cu, st);
     else if (a.S > 1) launch_combine(a, D, rows, st);
     if (with_scores) {
         // Eq. 1 over history rounds and, for several query tokens, the visible part of the question itself
@@ -185,16 +196,16 @@ extern "C" int ra_round_sparse_attn_prefill(ra_ctx* ctx, void* stream, const voi
                                             const ra_kv_view* layer, const int32_t* sel_idx, const int32_t* n_sel,
                                             const void* cur_k, const void* cur_v, int cur_len, float scale, float* out,
                                             float* lse) {
-    return prefill_impl(ctx, stream, q, q_len, Hq, layer, sel_idx, n_sel, cur_k, cur_v, cur_len, scale, out, lse, nullptr,
-                        nullptr);
+    return question_attention(ctx, "prefill", stream, q, q_len, Hq, layer, sel_idx, n_sel, cur_k, cur_v, cur_len, scale, out, lse,
+                              nullptr, nullptr, nullptr);
 }
 
 extern "C" int ra_watershed_attn_prefill(ra_ctx* ctx, void* stream, const void* q, int q_len, int Hq,
                                          const ra_kv_view* watershed, const void* cur_k, const void* cur_v, int cur_len,
                                          float scale, float* out, float* lse, float* scores_head, float* scores) {
     RA_REQUIRE(scores != nullptr, RA_ERR_INVALID_ARG, "watershed prefill: scores is NULL");
-    return prefill_impl(ctx, stream, q, q_len, Hq, watershed, nullptr, nullptr, cur_k, cur_v, cur_len, scale, out, lse,
-                        scores_head, scores);
+    return question_attention(ctx, "prefill", stream, q, q_len, Hq, watershed, nullptr, nullptr, cur_k, cur_v, cur_len, scale, out,
+                              lse, scores_head, scores, nullptr);
 }
 
 extern "C" int ra_set_prefill_precision(ra_ctx* ctx, int mode) {
