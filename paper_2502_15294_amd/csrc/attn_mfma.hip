@@ -658,8 +658,15 @@ __global__ __launch_bounds__(256, 2) void attn_mfma_kernel(AttnArgs a, int n_row
                 // (the compiler's iterative-ilp schedule, which the tests compare with, crashes on 64 channels without the fence)
                 if (D == 64) __builtin_amdgcn_sched_barrier(0);
                 uint4 ph[kParts];
+                if constexpr (TREE && D == 128) {  // both parts to the nearest: a weight is off by 2^-18 of itself at most, of either sign
+                    ph[0] = make_uint4(pack_nearest(p[0], p[1]), pack_nearest(p[2], p[3]), pack_nearest(p[4], p[5]), pack_nearest(p[6], p[7]));
+                    ph[1] = make_uint4(pack_nearest(p[0] - low_bf16(ph[0].x), p[1] - high_bf16(ph[0].x)),
+                                       pack_nearest(p[2] - low_bf16(ph[0].y), p[3] - high_bf16(ph[0].y)),
+                                       pack_nearest(p[4] - low_bf16(ph[0].z), p[5] - high_bf16(ph[0].z)),
+                                       pack_nearest(p[6] - low_bf16(ph[0].w), p[7] - high_bf16(ph[0].w)));
+                }
 #pragma unroll
-                for (int i = 0; i < kParts; ++i) {
+                for (int i = 0; i < kParts && !(TREE && D == 128); ++i) {
                     ph[i].x = pack_trunc(p[0], p[1]);
                     ph[i].y = pack_trunc(p[2], p[3]);
                     ph[i].z = pack_trunc(p[4], p[5]);

@@ -454,6 +454,14 @@ __global__ __launch_bounds__(256, kWorkgroupsPerCuP) void attn_prefill_mfma_kern
                 } else {
                     const float ps = ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
                     l[nt] += ps;
+                    if constexpr (TREE) {  // both parts to the nearest: a weight is off by 2^-18 of itself at most, of either sign
+                        phi = make_uint4(pack_nearest(p[0], p[1]), pack_nearest(p[2], p[3]), pack_nearest(p[4], p[5]), pack_nearest(p[6], p[7]));
+                        plo = make_uint4(pack_nearest(p[0] - low_bf16(phi.x), p[1] - high_bf16(phi.x)),
+                                         pack_nearest(p[2] - low_bf16(phi.y), p[3] - high_bf16(phi.y)),
+                                         pack_nearest(p[4] - low_bf16(phi.z), p[5] - high_bf16(phi.z)),
+                                         pack_nearest(p[6] - low_bf16(phi.w), p[7] - high_bf16(phi.w)));
+                        return;
+                    }
                     phi.x = pack_hi16(p[0], p[1]);
                     phi.y = pack_hi16(p[2], p[3]);
                     phi.z = pack_hi16(p[4], p[5]);

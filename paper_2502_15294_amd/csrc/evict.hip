@@ -25,18 +25,40 @@ struct SelectTokensArgs {
 };
 
 constexpr int kSelThreads = 1024, kSelWaves = kSelThreads / 64;
-constexpr int kDigit = 11, kBins = 1 << kDigit;  // three passes: 11, 11 and 10 bits of the key
+constexpr int kDigit = 11, kBins = 1 << kDigit;  // three digits: 11, 11 and 10 bits of the key
+constexpr int kChunk = 256;                      // positions that a wave reads with one instruction: four a lane
+constexpr int kChunks = 8;                       // ... that it has in flight
+constexpr int kCandidates = 8192;                // keys that share the first digit with the threshold and fit into LDS
+
+typedef float float4_any __attribute__((ext_vector_type(4), aligned(4)));
+
+// One more of `bin` for every lane of the wave that has one: lanes that agree with the first of them are added up before (weights
+// of zero, which whole rounds have, would otherwise queue at one address).
+__device__ __forceinline__ void count_bin(int* hist, bool has, int bin) {
+    const unsigned long long all = __ballot(has);
+    if (!all) return;
+    const int lane = threadIdx.x & 63, leader = __ffsll(all) - 1, common = __builtin_amdgcn_readlane(bin, leader);
+    const unsigned long long same = __ballot(has && bin == common);
+    if (lane == leader) atomicAdd(&hist[common], __popcll(same));
+    else if (has && bin != common) atomicAdd(&hist[bin], 1);
+}
 
 // One workgroup per sequence.  The `need` largest weights of the middle (what is neither among the first nor the last tokens) are
-// those above a threshold key, found digit by digit from counts of the candidates that share the digits before, and, of those
-// equal to it, the first ones.  Then every wave takes a contiguous sixteenth of the positions: it counts what it keeps, and
-// writes it behind what the waves before it keep.  Counts are whole numbers: their order does not matter.
+// those above a threshold key and, of those equal to it, the first ones.  The threshold is found digit by digit from counts of
+// the candidates that share the digits before: over the weights for the first digit; the candidates that share it then lie in
+// LDS as a rule, and the other digits are counted there (if they are more, over the weights).
+// Every wave has a contiguous sixteenth of the positions: it knows how many of them it keeps, and writes them behind what the
+// waves before it keep.  Counts are whole numbers: their order does not matter.
+//
+// Bound by a compute unit's share of the cache bandwidth and its round trips: three passes over the weights, 2 KB a wave and
+// instruction group in flight.
 __global__ __launch_bounds__(kSelThreads) void select_tokens_kernel(SelectTokensArgs a) {
     __shared__ int s_hist[kBins];
     __shared__ int s_start[kMaxRounds + 1], s_below[kMaxRounds + 1];
-    __shared__ int s_wave[kSelWaves][2];
+    __shared__ int s_wave[kSelWaves][2];  // positions that are kept for certain, positions with the threshold's key
+    __shared__ uint2 s_cand[kCandidates];  // key, position
     __shared__ uint32_t s_digit;
-    __shared__ int s_left, s_total;
+    __shared__ int s_left, s_count, s_total;
     const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const float* w = a.weights + (size_t)b * a.n_pos;
     const int n_rounds = min(max(a.n_rounds[b], 0), a.R_max);
@@ -51,68 +73,174 @@ __global__ __launch_bounds__(kSelThreads) void select_tokens_kernel(SelectTokens
         }
         if (lane == 0) s_start[a.R_max] = s_total = before;
     }
+    for (int i = tid; i < kBins; i += kSelThreads) s_hist[i] = 0;
+    if (tid < kSelWaves) s_wave[tid][0] = s_wave[tid][1] = 0;
+    if (tid == 0) s_count = 0;
     __syncthreads();
     const int n = s_total, K = min(a.budget, n);
     const int first = min(a.keep_first, n), last = min(a.keep_last, n - first);
     const int lo = first, hi = n - last, need = K - first - last;  // of the positions lo .. hi - 1
 
+    // The wave's positions, kChunk at a time: f(first position of the chunk, the lane's four weights).  Past the end: zeros.
+    const int chunks = (n + kChunk - 1) / kChunk, c_lo = chunks * wave / kSelWaves, c_hi = chunks * (wave + 1) / kSelWaves;
+    auto each_chunk = [&](auto f) {
+        for (int c0 = c_lo; c0 < c_hi; c0 += kChunks) {
+            float x[kChunks][4];
+#pragma unroll
+            for (int j = 0; j < kChunks; ++j) {
+                const int p = (c0 + j) * kChunk + lane * 4;
+                float4_any v = {0.f, 0.f, 0.f, 0.f};
+                if (c0 + j < c_hi) {
+                    if (p + 4 <= n) {
+                        v = *reinterpret_cast<const float4_any*>(w + p);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 3; ++e)
+                            if (p + e < n) v[e] = w[p + e];
+                    }
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[j][e] = v[e];
+            }
+#pragma unroll
+            for (int j = 0; j < kChunks; ++j)
+                if (c0 + j < c_hi) f((c0 + j) * kChunk, x[j]);
+        }
+    };
+    // The digit at which the counts, from the largest one down, reach `left`; what is left of it then, and the candidates there.
+    auto find_digit = [&](int bits, int left) {
+        if (wave == 0) {
+            int taken = 0;
+            for (int i0 = (1 << bits) - 64; i0 >= 0; i0 -= 64) {
+                const int bin = i0 + 63 - lane, c = s_hist[bin], incl = wave_inclusive_sum(c);
+                const unsigned long long reached = __ballot(taken + incl >= left);
+                if (reached) {
+                    if (lane == __ffsll(reached) - 1) {
+                        s_digit = (uint32_t)bin;
+                        s_left = left - (taken + incl - c);
+                        s_total = c;
+                    }
+                    break;
+                }
+                taken += __builtin_amdgcn_readlane(incl, 63);
+            }
+        }
+        __syncthreads();
+    };
+    auto clear_bins = [&] {
+        for (int i = tid; i < kBins; i += kSelThreads) s_hist[i] = 0;
+        __syncthreads();
+    };
+
     uint32_t threshold = 0;  // keys above it are kept, and the first `equal` of those equal to it
     int equal = 0;
-    if (need > 0 && need < hi - lo) {
-        int left = need;
-        for (int shift = 32 - kDigit; ; shift = max(shift - kDigit, 0)) {
-            // (the last digit is shorter: its upper bits are part of the one before)
-            const int bits = shift == 32 - kDigit ? kDigit : shift > 0 ? kDigit : 32 - 2 * kDigit;
-            for (int i = tid; i < kBins; i += kSelThreads) s_hist[i] = 0;
-            __syncthreads();
-            const int above = shift + bits;
-            for (int p = lo + tid; p < hi; p += kSelThreads) {
-                const uint32_t key = weight_key(w[p]);
-                if (above == 32 || key >> above == threshold >> above) atomicAdd(&s_hist[key >> shift & ((1u << bits) - 1)], 1);
-            }
-            __syncthreads();
-            if (wave == 0) {  // from the largest digit down: the first at which the count reaches what is left
-                int taken = 0;
-                for (int i0 = (1 << bits) - 64; i0 >= 0; i0 -= 64) {
-                    const int bin = i0 + 63 - lane, c = s_hist[bin], incl = wave_inclusive_sum(c);
-                    const unsigned long long reached = __ballot(taken + incl >= left);
-                    if (reached) {
-                        const int at = __ffsll(reached) - 1;
-                        if (lane == at) {
-                            s_digit = (uint32_t)bin;
-                            s_left = left - (taken + incl - c);
-                        }
-                        break;
-                    }
-                    taken += __builtin_amdgcn_readlane(incl, 63);
-                }
-            }
-            __syncthreads();
-            threshold |= s_digit << shift;
-            left = s_left;
-            if (shift == 0) break;
-        }
-        equal = left;
-    }
     const bool all = need >= hi - lo, none = need <= 0;
+    bool counted = false;  // s_wave is complete
+    if (!all && !none) {
+        constexpr int kShift1 = 32 - kDigit, kShift2 = kShift1 - kDigit;
+        each_chunk([&](int p0, const float (&x)[4]) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int p = p0 + lane * 4 + e;
+                count_bin(s_hist, p >= lo && p < hi, weight_key(x[e]) >> kShift1);
+            }
+        });
+        __syncthreads();
+        find_digit(kDigit, need);
+        const uint32_t digit1 = s_digit;
+        threshold = digit1 << kShift1;
+        int left = s_left;
+        const bool in_lds = s_total <= kCandidates;
+        clear_bins();
+        if (in_lds) {
+            int sure = 0;
+            each_chunk([&](int p0, const float (&x)[4]) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int p = p0 + lane * 4 + e;
+                    const uint32_t key = weight_key(x[e]), digit = key >> kShift1;
+                    const bool middle = p >= lo && p < hi;
+                    sure += __popcll(__ballot(p < n && (!middle || digit > digit1)));
+                    const unsigned long long take = __ballot(middle && digit == digit1);
+                    if (!take) continue;
+                    int at = 0;
+                    if (lane == 0) at = atomicAdd(&s_count, __popcll(take));
+                    at = __builtin_amdgcn_readfirstlane(at) + __popcll(take & ((1ull << lane) - 1));
+                    if (take >> lane & 1) s_cand[at] = make_uint2(key, (uint32_t)p);
+                }
+            });
+            if (lane == 0) s_wave[wave][0] = sure;
+            __syncthreads();
+            const int n_cand = s_count;
+            for (int i = tid; i < n_cand; i += kSelThreads) atomicAdd(&s_hist[s_cand[i].x >> kShift2 & (kBins - 1)], 1);
+            __syncthreads();
+            find_digit(kDigit, left);
+            threshold |= s_digit << kShift2;
+            left = s_left;
+            clear_bins();
+            for (int i = tid; i < n_cand; i += kSelThreads)
+                if (s_cand[i].x >> kShift2 == threshold >> kShift2) atomicAdd(&s_hist[s_cand[i].x & ((1 << kShift2) - 1)], 1);
+            __syncthreads();
+            find_digit(kShift2, left);
+            threshold |= s_digit;
+            equal = s_left;
+            for (int i = tid; i < n_cand; i += kSelThreads) {
+                if (s_cand[i].x < threshold) continue;
+                // the wave whose positions these are: the last one that begins at or before the chunk
+                const int c = (int)s_cand[i].y / kChunk;
+                int owner = (int)(((long long)c * kSelWaves) / chunks);
+                while (owner + 1 < kSelWaves && chunks * (owner + 1) / kSelWaves <= c) ++owner;
+                atomicAdd(&s_wave[owner][s_cand[i].x == threshold], 1);
+            }
+            counted = true;
+        } else {
+            each_chunk([&](int p0, const float (&x)[4]) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int p = p0 + lane * 4 + e;
+                    const uint32_t key = weight_key(x[e]);
+                    count_bin(s_hist, p >= lo && p < hi && key >> kShift1 == digit1, key >> kShift2 & (kBins - 1));
+                }
+            });
+            __syncthreads();
+            find_digit(kDigit, left);
+            threshold |= s_digit << kShift2;
+            left = s_left;
+            clear_bins();
+            each_chunk([&](int p0, const float (&x)[4]) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int p = p0 + lane * 4 + e;
+                    const uint32_t key = weight_key(x[e]);
+                    count_bin(s_hist, p >= lo && p < hi && key >> kShift2 == threshold >> kShift2, key & ((1 << kShift2) - 1));
+                }
+            });
+            __syncthreads();
+            find_digit(kShift2, left);
+            threshold |= s_digit;
+            equal = s_left;
+        }
+    }
     // 0: dropped, 1: kept, 2: kept if it is among the first `equal` of its kind
     auto fate = [&](int p, float x) {
-        if (p >= n) return 0;
-        if (p < lo || p >= hi || all) return 1;
-        if (none) return 0;
         const uint32_t key = weight_key(x);
-        return key > threshold ? 1 : key == threshold ? 2 : 0;
+        const int of_middle = all ? 1 : none ? 0 : key > threshold ? 1 : key == threshold ? 2 : 0;
+        return p >= n ? 0 : p < lo || p >= hi ? 1 : of_middle;
     };
-    const int chunks = (n + 63) / 64, c_lo = chunks * wave / kSelWaves, c_hi = chunks * (wave + 1) / kSelWaves;
-    int n_sure = 0, n_equal = 0;
-    for (int c = c_lo; c < c_hi; ++c) {
-        const int p = c * 64 + lane, f = fate(p, p < n ? w[p] : 0.f);
-        n_sure += __popcll(__ballot(f == 1));
-        n_equal += __popcll(__ballot(f == 2));
-    }
-    if (lane == 0) {
-        s_wave[wave][0] = n_sure;
-        s_wave[wave][1] = n_equal;
+    if (!counted) {
+        int n_sure = 0, n_equal = 0;
+        each_chunk([&](int p0, const float (&x)[4]) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int f = fate(p0 + lane * 4 + e, x[e]);
+                n_sure += __popcll(__ballot(f == 1));
+                n_equal += __popcll(__ballot(f == 2));
+            }
+        });
+        if (lane == 0) {
+            s_wave[wave][0] = n_sure;
+            s_wave[wave][1] = n_equal;
+        }
     }
     __syncthreads();
     int at = 0, equal_before = 0;
@@ -125,37 +253,54 @@ __global__ __launch_bounds__(kSelThreads) void select_tokens_kernel(SelectTokens
     float* left_over = a.kept_weights ? a.kept_weights + (size_t)b * a.n_pos : nullptr;
     // the round whose start comes next: the first that starts at or behind this wave's part (the first wave: round 0)
     int round = 0;
-    if (c_lo < c_hi) {
-        for (int r0 = 0; r0 <= a.R_max; r0 += 64)
-            round += __popcll(__ballot(r0 + lane <= a.R_max && s_start[min(r0 + lane, a.R_max)] < c_lo * 64));
-    }
+    for (int r0 = 0; r0 <= a.R_max; r0 += 64)
+        round += __popcll(__ballot(r0 + lane <= a.R_max && s_start[min(r0 + lane, a.R_max)] < c_lo * kChunk));
     const unsigned long long below_lane = (1ull << lane) - 1;
-    for (int c = c_lo; c < c_hi; ++c) {
-        const int p = c * 64 + lane;
-        const float x = p < n ? w[p] : 0.f;
-        const int f = fate(p, x);
-        const unsigned long long maybe = __ballot(f == 2);
-        const unsigned long long kept = __ballot(f == 1 || (f == 2 && equal_before + __popcll(maybe & below_lane) < equal));
-        while (round <= a.R_max && s_start[round] < c * 64 + 64) {
-            const int in = s_start[round] - c * 64;
-            if (lane == 0) s_below[round] = at + __popcll(kept & ((1ull << in) - 1));
+    each_chunk([&](int p0, const float (&x)[4]) {
+        // positions in order: lane by lane, four each
+        unsigned long long kept[4], maybe[4];
+        int f[4], eq = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            f[e] = fate(p0 + lane * 4 + e, x[e]);
+            maybe[e] = __ballot(f[e] == 2);
+            eq += __popcll(maybe[e] & below_lane);
+        }
+        eq += equal_before;
+        int j = at;
+        bool mine[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            mine[e] = f[e] == 1 || (f[e] == 2 && eq < equal);
+            eq += f[e] == 2;
+            kept[e] = __ballot(mine[e]);
+            j += __popcll(kept[e] & below_lane);
+        }
+        while (round <= a.R_max && s_start[round] < p0 + kChunk) {
+            const int in = s_start[round] - p0, in_lane = in >> 2, in_e = in & 3;
+            int below = at;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) below += __popcll(kept[e] & ((1ull << in_lane) - 1)) + (e < in_e && (kept[e] >> in_lane & 1));
+            if (lane == 0) s_below[round] = below;
             ++round;
         }
-        if (kept >> lane & 1) {
-            const int j = at + __popcll(kept & below_lane);
-            idx[j] = p;
-            if (left_over) left_over[j] = x;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (mine[e]) {
+                idx[j] = p0 + lane * 4 + e;
+                if (left_over) left_over[j] = x[e];
+                ++j;
+            }
+            at += __popcll(kept[e]);
+            equal_before += __popcll(maybe[e]);
         }
-        at += __popcll(kept);
-        equal_before += __popcll(maybe);
-    }
+    });
     for (int j = K + tid; j < a.budget; j += kSelThreads) idx[j] = -1;
     if (left_over)
         for (int j = K + tid; j < a.n_pos; j += kSelThreads) left_over[j] = 0.f;
-    __syncthreads();
-    // starts behind the last whole chunk (and all of them, if there are no tokens): everything kept lies below
+    // starts behind the last chunk (and all of them, if there are no tokens): everything kept lies below
     for (int r = tid; r <= a.R_max; r += kSelThreads)
-        if (s_start[r] >= chunks * 64) s_below[r] = K;
+        if (s_start[r] >= chunks * kChunk) s_below[r] = K;
     __syncthreads();
     if (wave == 0) {
         long long off = (long long)b * a.stride;
@@ -179,92 +324,174 @@ struct CompactArgs {
     int max_kept;
 };
 
-template <typename T, int D>
-__device__ __forceinline__ size_t key_row(const DevView& v, int b, long long off, int len, int g, int t) {
-    if (v.block_size) {
-        const long long at = min(max(off + t / 16, 0ll), (long long)v.max_blocks - 1);
-        return ((size_t)max(v.block_table[(size_t)b * v.max_blocks + at], 0) * v.Hkv + g) * 16 + t % 16;
-    }
-    return (size_t)off * v.Hkv + (size_t)g * len + t;
-}
-// First element of the value tile that holds token t.
-template <typename T, int D>
-__device__ __forceinline__ size_t value_tile(const DevView& v, int b, long long off_k, long long off_v, int len, int g, int t) {
-    if (v.block_size) {
-        const long long at = min(max(off_k + t / 16, 0ll), (long long)v.max_blocks - 1);
-        return ((size_t)max(v.block_table[(size_t)b * v.max_blocks + at], 0) * v.Hkv + g) * D * 16;
-    }
-    return ((size_t)off_v * v.Hkv + (size_t)g * ((len + 15) & ~15) + (t & ~15)) * D;
-}
+constexpr int kCompactTokens = 128;  // kept tokens that a workgroup moves: eight tiles, of one round
 
-// grid (value tiles of a sequence's smaller cache, B): a workgroup makes one tile of 16 tokens for every KV head, a wave a
-// head at a time.
+// Where the tokens of a round lie: key row and first element of the value tile, for head 0, and from one head to the next.
+struct RoundPlace {
+    const DevView& v;
+    int b, len;
+    long long off, off_v;
+    __device__ __forceinline__ RoundPlace(const DevView& view, int b_, int round, int len_) : v(view), b(b_), len(len_) {
+        off = v.seg_off[(size_t)b * v.R_max + round];
+        off_v = v.seg_off_v[(size_t)b * v.R_max + round];
+    }
+    __device__ __forceinline__ long long block(int t) const {
+        const long long at = min(max(off + t / 16, 0ll), (long long)v.max_blocks - 1);
+        return (long long)max(v.block_table[(size_t)b * v.max_blocks + at], 0) * v.Hkv;
+    }
+    __device__ __forceinline__ long long key_row(int t) const { return v.block_size ? block(t) * 16 + t % 16 : off * v.Hkv + t; }
+    __device__ __forceinline__ long long value_tile(int t, int d) const {
+        return v.block_size ? block(t) * 16 * d : (off_v * v.Hkv + (t & ~15)) * d;
+    }
+    __device__ __forceinline__ int key_stride() const { return v.block_size ? 16 : len; }
+    __device__ __forceinline__ int value_stride(int d) const { return v.block_size ? 16 * d : ((len + 15) & ~15) * d; }
+};
+
+// grid (pieces of kCompactTokens of a sequence's rounds, B).  A wave moves the keys or the values of one head at a time.
+// Keys are rows.  Values are tiles of 16 tokens, [D][16], of which a kept token is a column: a wave has the source tile that the
+// next kept tokens lie in in LDS and the one after that on its way, a lane owns channels and picks the columns of its new tile
+// one by one, so that every source tile is read once, as whole cache lines, and every new one written once.  (With a load per
+// element, 64 channels in 64 sectors of a tile, 2 GB moved in 663 microseconds, the second-level cache read eight times over.)
 template <typename T, int D>
 __global__ __launch_bounds__(256) void compact_rounds_kernel(CompactArgs a) {
     constexpr int kPieces = D * sizeof(T) / 16;  // of a key row
+    constexpr int kQuads = (int)sizeof(T), kChannels = D / 64;  // 16-byte pieces of a channel's 16 tokens; channels of a lane
+    constexpr int kPitch = 4 * kQuads + 2;  // 32-bit words of a channel in LDS: 16 tokens, then zeros for tokens from nowhere
+    __shared__ long long s_key[kCompactTokens], s_tile[kCompactTokens], s_new_key[kCompactTokens], s_new_tile[kCompactTokens / 16];
+    __shared__ int s_from[kCompactTokens], s_next[kCompactTokens];  // source token (-1: none); first later one of another tile
+    __shared__ __align__(16) uint32_t s_column[4][D * kPitch];
     const int b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int R = a.src.R_max, n_src = min(max(a.src.n_rounds[b], 0), R), n_dst = min(max(a.dst.n_rounds[b], 0), R);
     const size_t row = (size_t)b * R;
-    // the tile's round: its lengths in both caches, and what lies before it
-    int round = -1, tile = 0, len = 0, first = 0, src_len = 0, src_first = 0;
+    // the piece's round: its lengths in both caches, and what lies before it (every wave for itself)
+    int round = -1, t0 = 0, len = 0, first = 0, src_len = 0, src_first = 0;
     {
-        int tiles_before = 0, dst_before = 0, src_before = 0;
+        int pieces_before = 0, dst_before = 0, src_before = 0;
         for (int r0 = 0; r0 < n_dst && round < 0; r0 += 64) {
             const int r = r0 + lane;
             const int d = r < n_dst ? max(a.dst.seg_len[row + r], 0) : 0, s = r < n_src ? max(a.src.seg_len[row + r], 0) : 0;
-            const int tiles = (d + 15) / 16;
-            const int tile_end = wave_inclusive_sum(tiles), d_end = wave_inclusive_sum(d), s_end = wave_inclusive_sum(s);
-            const int target = (int)blockIdx.x - tiles_before;
-            const unsigned long long in = __ballot(tile_end > target && tile_end - tiles <= target);
+            const int pieces = (d + kCompactTokens - 1) / kCompactTokens;
+            const int end = wave_inclusive_sum(pieces), d_end = wave_inclusive_sum(d), s_end = wave_inclusive_sum(s);
+            const int target = (int)blockIdx.x - pieces_before;
+            const unsigned long long in = __ballot(end > target && end - pieces <= target);
             if (in) {
                 const int at = __ffsll(in) - 1;
                 round = r0 + at;
                 len = __builtin_amdgcn_readlane(d, at);
                 src_len = __builtin_amdgcn_readlane(s, at);
-                tile = target - (__builtin_amdgcn_readlane(tile_end, at) - __builtin_amdgcn_readlane(tiles, at));
+                t0 = (target - (__builtin_amdgcn_readlane(end, at) - __builtin_amdgcn_readlane(pieces, at))) * kCompactTokens;
                 first = dst_before + __builtin_amdgcn_readlane(d_end, at) - len;
                 src_first = src_before + __builtin_amdgcn_readlane(s_end, at) - src_len;
             }
-            tiles_before += __builtin_amdgcn_readlane(tile_end, 63);
+            pieces_before += __builtin_amdgcn_readlane(end, 63);
             dst_before += __builtin_amdgcn_readlane(d_end, 63);
             src_before += __builtin_amdgcn_readlane(s_end, 63);
         }
     }
     if (round < 0) return;
-    // lane % 16: the tile's token, and where it comes from (-1: nowhere)
-    const int t = tile * 16 + (lane & 15), j = first + t;
-    int from = -1;
-    if (t < len && j < min(max(a.n_kept[b], 0), a.max_kept)) {
-        from = a.kept_idx[(size_t)b * a.max_kept + j] - src_first;
-        if (from < 0 || from >= src_len) from = -1;
-    }
-    const long long so = a.src.seg_off[row + round], sv = a.src.seg_off_v[row + round];
-    const long long dof = a.dst.seg_off[row + round], dv = a.dst.seg_off_v[row + round];
-    const int Hkv = a.src.Hkv;
-    for (int g = wave; g < Hkv; g += 4) {
-        for (int x = lane; x < 16 * kPieces; x += 64) {
-            const int i = x / kPieces, c = x % kPieces, src_t = __shfl(from, i, 64);
-            if (tile * 16 + i >= len) continue;
-            uint4 k = make_uint4(0, 0, 0, 0);
-            if (src_t >= 0)
-                k = reinterpret_cast<const uint4*>(static_cast<const T*>(a.src.k) + key_row<T, D>(a.src, b, so, src_len, g, src_t) * D)[c];
-            reinterpret_cast<uint4*>(static_cast<T*>(const_cast<void*>(a.dst.k)) + key_row<T, D>(a.dst, b, dof, len, g, tile * 16 + i) * D)[c] = k;
+    const RoundPlace src(a.src, b, round, src_len), dst(a.dst, b, round, len);
+    const int here = min(kCompactTokens, len - t0);
+    if (tid < kCompactTokens) {
+        const int j = first + t0 + tid;
+        int from = -1;
+        if (tid < here && j < min(max(a.n_kept[b], 0), a.max_kept)) {
+            from = a.kept_idx[(size_t)b * a.max_kept + j] - src_first;
+            if (from < 0 || from >= src_len) from = -1;
         }
-        if (a.src.v == nullptr) continue;
-        T* out = static_cast<T*>(const_cast<void*>(a.dst.v)) + value_tile<T, D>(a.dst, b, dof, dv, len, g, tile * 16);
-        const size_t my_tile = from >= 0 ? value_tile<T, D>(a.src, b, so, sv, src_len, g, from) + (from & 15) : 0;
-        for (int c = lane; c < D; c += 64) {
-            union {
-                T e[16];
-                uint4 u[sizeof(T)];
-            } v;
+        s_from[tid] = from;
+        if (from >= 0) {
+            s_key[tid] = src.key_row(from);
+            s_tile[tid] = src.value_tile(from, D);
+        }
+        if (tid < here) s_new_key[tid] = dst.key_row(t0 + tid);
+        if (tid % 16 == 0 && tid < here) s_new_tile[tid / 16] = dst.value_tile(t0 + tid, D);
+    }
+    __syncthreads();
+    if (tid < kCompactTokens) {
+        int k = tid + 1;  // (a token that comes from nowhere needs no tile)
+        while (k < here && (s_from[k] < 0 || s_from[k] >> 4 == s_from[tid] >> 4)) ++k;
+        s_next[tid] = k;
+    }
+    __syncthreads();
+    const int Hkv = a.src.Hkv;
+    const int jobs = a.src.v ? 2 * Hkv : Hkv;
+    for (int job = blockIdx.z * 4 + wave; job < jobs; job += 4 * gridDim.z) {
+        const int g = job >= Hkv ? job - Hkv : job;
+        if (job < Hkv) {
+            constexpr int kRows = 64 / kPieces, kFlight = 8;  // rows of an instruction; instructions in flight
+            const uint4* from = static_cast<const uint4*>(a.src.k);
+            uint4* to = static_cast<uint4*>(const_cast<void*>(a.dst.k));
+            const long long head = (long long)g * src.key_stride(), new_head = (long long)g * dst.key_stride();
+            for (int i0 = 0; i0 < here; i0 += kRows * kFlight) {
+                uint4 k[kFlight];
+#pragma unroll
+                for (int f = 0; f < kFlight; ++f) {
+                    const int i = i0 + f * kRows + lane / kPieces;
+                    k[f] = make_uint4(0, 0, 0, 0);
+                    if (i < here && s_from[i] >= 0) k[f] = from[(s_key[i] + head) * kPieces + lane % kPieces];
+                }
+#pragma unroll
+                for (int f = 0; f < kFlight; ++f) {
+                    const int i = i0 + f * kRows + lane / kPieces;
+                    if (i < here) to[(s_new_key[i] + new_head) * kPieces + lane % kPieces] = k[f];
+                }
+            }
+            continue;
+        }
+        const T* from = static_cast<const T*>(a.src.v) + (size_t)g * src.value_stride(D) + lane * 16;
+        T* to = static_cast<T*>(const_cast<void*>(a.dst.v)) + (size_t)g * dst.value_stride(D) + lane * 16;
+        auto uniform = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
+        uint4 then[kChannels][kQuads];
+        auto load = [&](int i) {
+            const T* tile = from + s_tile[i];
+#pragma unroll
+            for (int c = 0; c < kChannels; ++c)
+#pragma unroll
+                for (int w = 0; w < kQuads; ++w) then[c][w] = reinterpret_cast<const uint4*>(tile + c * 1024)[w];
+        };
+        uint32_t* mine = s_column[wave] + lane * kPitch;  // of the lane's first channel; the second lies 64 * kPitch behind it
+        const T* columns = reinterpret_cast<const T*>(mine);
+#pragma unroll
+        for (int c = 0; c < kChannels; ++c) mine[c * 64 * kPitch + 4 * kQuads] = 0;
+        int next = 0;  // token whose tile is on its way
+        while (next < here && uniform(s_from[next]) < 0) ++next;
+        if (next < here) load(next);
+        for (int i0 = 0; i0 < here; i0 += 16) {
+            uint32_t out[kChannels][4 * kQuads];
+            const int from16 = s_from[i0 + (lane & 15)];
+            int column[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                const size_t at = ((size_t)(unsigned)__shfl((int)(my_tile >> 32), i, 64) << 32) | (unsigned)__shfl((int)my_tile, i, 64);
-                v.e[i] = __shfl(from, i, 64) >= 0 ? static_cast<const T*>(a.src.v)[at + c * 16] : T(0);
+                const int f = __builtin_amdgcn_readlane(from16, i);
+                column[i] = f < 0 ? 16 : f & 15;  // (behind the last token: none)
             }
 #pragma unroll
-            for (int i = 0; i < (int)sizeof(T); ++i) reinterpret_cast<uint4*>(out + c * 16)[i] = v.u[i];
+            for (int i = 0; i < 16; ++i) {
+                if (i0 + i == next) {
+#pragma unroll
+                    for (int c = 0; c < kChannels; ++c)
+#pragma unroll
+                        for (int w = 0; w < kQuads; ++w) {
+                            uint2* at = reinterpret_cast<uint2*>(mine + c * 64 * kPitch + 4 * w);
+                            at[0] = make_uint2(then[c][w].x, then[c][w].y);
+                            at[1] = make_uint2(then[c][w].z, then[c][w].w);
+                        }
+                    next = uniform(s_next[next]);
+                    if (next < here) load(next);
+                }
+#pragma unroll
+                for (int c = 0; c < kChannels; ++c) {
+                    const uint32_t x = columns[c * 64 * kPitch * (4 / sizeof(T)) + column[i]];
+                    if constexpr (sizeof(T) == 4) out[c][i] = x;
+                    else out[c][i / 2] = i % 2 ? out[c][i / 2] | x << 16 : x;
+                }
+            }
+            T* tile = to + s_new_tile[i0 / 16];
+#pragma unroll
+            for (int c = 0; c < kChannels; ++c)
+#pragma unroll
+                for (int w = 0; w < kQuads; ++w)
+                    reinterpret_cast<uint4*>(tile + c * 1024)[w] = make_uint4(out[c][4 * w], out[c][4 * w + 1], out[c][4 * w + 2], out[c][4 * w + 3]);
         }
     }
 }
@@ -328,6 +555,7 @@ extern "C" int ra_compact_rounds(ra_ctx* ctx, void* stream, const ra_kv_view* sr
                "compact_rounds: dst needs memory of its own");
     RA_REQUIRE(src->d == 64 || src->d == 128, RA_ERR_UNSUPPORTED, "compact_rounds: head_dim %d not in {64, 128}", src->d);
     RA_REQUIRE(src->B <= 65535, RA_ERR_UNSUPPORTED, "compact_rounds: batch %d exceeds 65535", src->B);
+    RA_REQUIRE(src->Hkv <= 65535, RA_ERR_UNSUPPORTED, "compact_rounds: Hkv %d exceeds 65535", src->Hkv);
     RA_REQUIRE((((uintptr_t)src->k | (uintptr_t)src->v | (uintptr_t)dst->k | (uintptr_t)dst->v) & 15) == 0, RA_ERR_INVALID_ARG,
                "compact_rounds: keys and values must be 16-byte aligned");
     CompactArgs a = {};
@@ -336,7 +564,7 @@ extern "C" int ra_compact_rounds(ra_ctx* ctx, void* stream, const ra_kv_view* sr
     a.kept_idx = kept_idx;
     a.n_kept = n_kept;
     a.max_kept = max_kept;
-    const dim3 grid((unsigned)(max_kept / 16 + src->R_max), (unsigned)src->B);
+    const dim3 grid((unsigned)(max_kept / kCompactTokens + src->R_max), (unsigned)src->B, (unsigned)((src->Hkv * (src->v ? 2 : 1) + 3) / 4));
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
     if (src->dtype == RA_BF16 && src->d == 128) hipLaunchKernelGGL((compact_rounds_kernel<uint16_t, 128>), grid, dim3(256), 0, st, a);
     else if (src->dtype == RA_BF16) hipLaunchKernelGGL((compact_rounds_kernel<uint16_t, 64>), grid, dim3(256), 0, st, a);

@@ -33,4 +33,13 @@ __device__ __forceinline__ uint32_t pack_hi16(float a, float b) {
 }
 __device__ __forceinline__ float trunc_bf16(float a) { return as_f32(as_u32(a) & 0xffff0000u); }
 
+// Two floats -> packed bf16 pair to the nearest (one v_cvt_pk_bf16_f32).
+__device__ __forceinline__ uint32_t pack_nearest(float a, float b) {
+    typedef float float2_t __attribute__((ext_vector_type(2)));
+    const float2_t f = {a, b};
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, bf16x2_t));
+}
+__device__ __forceinline__ float low_bf16(uint32_t pair) { return as_f32(pair << 16); }
+__device__ __forceinline__ float high_bf16(uint32_t pair) { return as_f32(pair & 0xffff0000u); }
+
 }  // namespace ra
