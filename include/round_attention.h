@@ -424,7 +424,7 @@ int ra_select_tokens(ra_ctx* ctx, void* stream, const float* weights, int n_pos,
 /*
  * The smaller cache: keys and values of the kept tokens of one layer, packed into round blocks of the new lengths.
  *   src        the layer's view
- *   kept_idx   device int32 [B][max_kept], ascending positions in src;  n_kept device int32 [B] (ra_select_tokens)
+ *   kept_idx   device int32 [B][max_kept], strictly ascending positions in src;  n_kept device int32 [B] (ra_select_tokens)
  *   dst        view of the smaller cache: k and v (written; memory of their own, not overlapping src's), seg_off, seg_off_v,
  *              seg_len = kept_len (adding up to n_kept), n_rounds, block_table.  B, R_max, Hkv, d and dtype of src; either
  *              layout, whatever src's is

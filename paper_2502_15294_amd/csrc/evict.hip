@@ -348,17 +348,18 @@ struct RoundPlace {
 };
 
 // grid (pieces of kCompactTokens of a sequence's rounds, B).  A wave moves the keys or the values of one head at a time.
-// Keys are rows.  Values are tiles of 16 tokens, [D][16], of which a kept token is a column: a wave has the source tile that the
-// next kept tokens lie in in LDS and the one after that on its way, a lane owns channels and picks the columns of its new tile
-// one by one, so that every source tile is read once, as whole cache lines, and every new one written once.  (With a load per
-// element, 64 channels in 64 sectors of a tile, 2 GB moved in 663 microseconds, the second-level cache read eight times over.)
+// Keys are rows.  Values are tiles of 16 tokens, [D][16], of which a kept token is a column: a lane owns channels, has its rows of
+// two source tiles in registers or on their way, writes the columns that stay side by side into LDS, and from there every new
+// tile goes out once, as 32 (64) contiguous bytes a channel; every source tile is read once.  (With a load per element, 64
+// channels in 64 sectors of a tile, 2 GB moved in 663 microseconds, the second-level cache read eight times over.)
 template <typename T, int D>
 __global__ __launch_bounds__(256) void compact_rounds_kernel(CompactArgs a) {
     constexpr int kPieces = D * sizeof(T) / 16;  // of a key row
     constexpr int kQuads = (int)sizeof(T), kChannels = D / 64;  // 16-byte pieces of a channel's 16 tokens; channels of a lane
-    constexpr int kPitch = 4 * kQuads + 2;  // 32-bit words of a channel in LDS: 16 tokens, then zeros for tokens from nowhere
+    constexpr int kPitch = 8 * kQuads + 2;  // 32-bit words of a channel in LDS: 32 tokens
     __shared__ long long s_key[kCompactTokens], s_tile[kCompactTokens], s_new_key[kCompactTokens], s_new_tile[kCompactTokens / 16];
-    __shared__ int s_from[kCompactTokens], s_next[kCompactTokens];  // source token (-1: none); first later one of another tile
+    __shared__ int s_from[kCompactTokens];  // source token (-1: none)
+    __shared__ int s_mask[kCompactTokens], s_valid[kCompactTokens / 16];
     __shared__ __align__(16) uint32_t s_column[4][D * kPitch];
     const int b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int R = a.src.R_max, n_src = min(max(a.src.n_rounds[b], 0), R), n_dst = min(max(a.dst.n_rounds[b], 0), R);
@@ -399,18 +400,29 @@ __global__ __launch_bounds__(256) void compact_rounds_kernel(CompactArgs a) {
             if (from < 0 || from >= src_len) from = -1;
         }
         s_from[tid] = from;
-        if (from >= 0) {
-            s_key[tid] = src.key_row(from);
-            s_tile[tid] = src.value_tile(from, D);
-        }
+        s_key[tid] = from >= 0 ? src.key_row(from) : 0;
         if (tid < here) s_new_key[tid] = dst.key_row(t0 + tid);
         if (tid % 16 == 0 && tid < here) s_new_tile[tid / 16] = dst.value_tile(t0 + tid, D);
     }
     __syncthreads();
-    if (tid < kCompactTokens) {
-        int k = tid + 1;  // (a token that comes from nowhere needs no tile)
-        while (k < here && (s_from[k] < 0 || s_from[k] >> 4 == s_from[tid] >> 4)) ++k;
-        s_next[tid] = k;
+    // the source tiles that the piece takes columns of, one after the other: where, which columns, and the new place of the first
+    int n_tiles = 0;
+    if (a.src.v) {
+        auto tile_of = [&](int i) { return i >= 0 && i < here && s_from[i] >= 0 ? s_from[i] >> 4 : -1; };
+        for (int i0 = 0; i0 < here; i0 += 64) {
+            const int i = i0 + lane, tile = tile_of(i);
+            const unsigned long long starts = __ballot(tile >= 0 && tile != tile_of(i - 1));
+            if (wave == 0 && (starts >> lane & 1)) {
+                int mask = 0;
+                for (int j = i; j < here && tile_of(j) == tile; ++j) mask |= 1 << (s_from[j] & 15);
+                const int k = n_tiles + __popcll(starts & ((1ull << lane) - 1));
+                s_mask[k] = i << 16 | mask;
+                s_tile[k] = src.value_tile(s_from[i], D);
+            }
+            const unsigned long long some = __ballot(tile >= 0);
+            if (wave == 0 && lane < 4) s_valid[i0 / 16 + lane] = (int)(some >> 16 * lane & 0xffff);
+            n_tiles += __popcll(starts);
+        }
     }
     __syncthreads();
     const int Hkv = a.src.Hkv;
@@ -423,13 +435,19 @@ __global__ __launch_bounds__(256) void compact_rounds_kernel(CompactArgs a) {
             uint4* to = static_cast<uint4*>(const_cast<void*>(a.dst.k));
             const long long head = (long long)g * src.key_stride(), new_head = (long long)g * dst.key_stride();
             for (int i0 = 0; i0 < here; i0 += kRows * kFlight) {
+                const uint4* at[kFlight];
+                bool some[kFlight];
                 uint4 k[kFlight];
 #pragma unroll
                 for (int f = 0; f < kFlight; ++f) {
-                    const int i = i0 + f * kRows + lane / kPieces;
+                    const int i = min(i0 + f * kRows + lane / kPieces, kCompactTokens - 1);
+                    some[f] = s_from[i] >= 0;
+                    at[f] = from + (s_key[i] + head) * kPieces + lane % kPieces;
                     k[f] = make_uint4(0, 0, 0, 0);
-                    if (i < here && s_from[i] >= 0) k[f] = from[(s_key[i] + head) * kPieces + lane % kPieces];
                 }
+#pragma unroll
+                for (int f = 0; f < kFlight; ++f)
+                    if (some[f]) k[f] = load_once(at[f]);
 #pragma unroll
                 for (int f = 0; f < kFlight; ++f) {
                     const int i = i0 + f * kRows + lane / kPieces;
@@ -440,59 +458,77 @@ __global__ __launch_bounds__(256) void compact_rounds_kernel(CompactArgs a) {
         }
         const T* from = static_cast<const T*>(a.src.v) + (size_t)g * src.value_stride(D) + lane * 16;
         T* to = static_cast<T*>(const_cast<void*>(a.dst.v)) + (size_t)g * dst.value_stride(D) + lane * 16;
-        auto uniform = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
-        uint4 then[kChannels][kQuads];
-        auto load = [&](int i) {
-            const T* tile = from + s_tile[i];
+        struct Tile {  // the lane's channels (lane, lane + 64) of a source tile
+            uint32_t x[kChannels][4 * kQuads];
+        };
+        auto load = [&](int k) {
+            Tile t;
+            const T* tile = from + s_tile[min(k, n_tiles - 1)];
 #pragma unroll
             for (int c = 0; c < kChannels; ++c)
 #pragma unroll
-                for (int w = 0; w < kQuads; ++w) then[c][w] = reinterpret_cast<const uint4*>(tile + c * 1024)[w];
-        };
-        uint32_t* mine = s_column[wave] + lane * kPitch;  // of the lane's first channel; the second lies 64 * kPitch behind it
-        const T* columns = reinterpret_cast<const T*>(mine);
-#pragma unroll
-        for (int c = 0; c < kChannels; ++c) mine[c * 64 * kPitch + 4 * kQuads] = 0;
-        int next = 0;  // token whose tile is on its way
-        while (next < here && uniform(s_from[next]) < 0) ++next;
-        if (next < here) load(next);
-        for (int i0 = 0; i0 < here; i0 += 16) {
-            uint32_t out[kChannels][4 * kQuads];
-            const int from16 = s_from[i0 + (lane & 15)];
-            int column[16];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int f = __builtin_amdgcn_readlane(from16, i);
-                column[i] = f < 0 ? 16 : f & 15;  // (behind the last token: none)
-            }
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                if (i0 + i == next) {
-#pragma unroll
-                    for (int c = 0; c < kChannels; ++c)
-#pragma unroll
-                        for (int w = 0; w < kQuads; ++w) {
-                            uint2* at = reinterpret_cast<uint2*>(mine + c * 64 * kPitch + 4 * w);
-                            at[0] = make_uint2(then[c][w].x, then[c][w].y);
-                            at[1] = make_uint2(then[c][w].z, then[c][w].w);
-                        }
-                    next = uniform(s_next[next]);
-                    if (next < here) load(next);
+                for (int w = 0; w < kQuads; ++w) {
+                    const uint4 v = reinterpret_cast<const uint4*>(tile + c * 1024)[w];
+                    t.x[c][4 * w] = v.x, t.x[c][4 * w + 1] = v.y, t.x[c][4 * w + 2] = v.z, t.x[c][4 * w + 3] = v.w;
                 }
+            return t;
+        };
+        // the lane's channels of two new tiles, in turn: token j is column j % 32
+        uint32_t* mine = s_column[wave] + lane * kPitch;
+        T* columns = reinterpret_cast<T*>(mine);
+        constexpr int kNextChannel = 64 * kPitch;  // words to the lane's second channel
+        int written = 0;  // new tiles
+        auto write_out = [&](int upto) {  // the new tiles that end before token `upto`
+            while (written < upto >> 4) {
+                const int valid = __builtin_amdgcn_readfirstlane(s_valid[written]);
+                T* tile = to + s_new_tile[written];
 #pragma unroll
                 for (int c = 0; c < kChannels; ++c) {
-                    const uint32_t x = columns[c * 64 * kPitch * (4 / sizeof(T)) + column[i]];
-                    if constexpr (sizeof(T) == 4) out[c][i] = x;
-                    else out[c][i / 2] = i % 2 ? out[c][i / 2] | x << 16 : x;
+                    uint32_t x[4 * kQuads];
+#pragma unroll
+                    for (int w = 0; w < 2 * kQuads; ++w) {
+                        const uint2 v = *reinterpret_cast<const uint2*>(mine + c * kNextChannel + (written & 1) * 4 * kQuads + 2 * w);
+                        x[2 * w] = v.x, x[2 * w + 1] = v.y;
+                    }
+                    if (valid != 0xffff) {  // columns behind the round's end, and those that come from nowhere: zeros
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            if (!(valid >> i & 1)) x[i * (int)sizeof(T) / 4] &= sizeof(T) == 4 ? 0u : i % 2 ? 0x0000ffffu : 0xffff0000u;
+                    }
+#pragma unroll
+                    for (int w = 0; w < kQuads; ++w)
+                        reinterpret_cast<uint4*>(tile + c * 1024)[w] = make_uint4(x[4 * w], x[4 * w + 1], x[4 * w + 2], x[4 * w + 3]);
                 }
+                ++written;
             }
-            T* tile = to + s_new_tile[i0 / 16];
+        };
+        auto pick = [&](const Tile& t, int k) {  // the kept columns of source tile k
+            const int first_mask = __builtin_amdgcn_readfirstlane(s_mask[k]), first_j = first_mask >> 16;
+            write_out(first_j);
+            int j = first_j;
 #pragma unroll
-            for (int c = 0; c < kChannels; ++c)
+            for (int e = 0; e < 16; ++e)
+                if (first_mask >> e & 1) {
 #pragma unroll
-                for (int w = 0; w < kQuads; ++w)
-                    reinterpret_cast<uint4*>(tile + c * 1024)[w] = make_uint4(out[c][4 * w], out[c][4 * w + 1], out[c][4 * w + 2], out[c][4 * w + 3]);
+                    for (int c = 0; c < kChannels; ++c) {
+                        T* at = columns + c * kNextChannel * (4 / (int)sizeof(T)) + (j & 31);
+                        if constexpr (sizeof(T) == 4) *at = t.x[c][e];
+                        else *at = (T)(e % 2 ? t.x[c][e / 2] >> 16 : t.x[c][e / 2]);
+                    }
+                    ++j;
+                }
+        };
+        if (n_tiles > 0) {  // two tiles held, the request for the next one made in any case: no wait is for more than the tile in hand
+            Tile x = load(0), y;
+            for (int k = 0; k < n_tiles; k += 2) {
+                y = load(k + 1);
+                pick(x, k);
+                if (k + 1 >= n_tiles) break;
+                x = load(k + 2);
+                pick(y, k + 1);
+            }
         }
+        write_out((here + 15) & ~15);
     }
 }
 
