@@ -29,18 +29,239 @@ constexpr int kDigit = 11, kBins = 1 << kDigit;  // three digits: 11, 11 and 10 
 constexpr int kChunk = 256;                      // positions that a wave reads with one instruction: four a lane
 constexpr int kChunks = 8;                       // ... that it has in flight
 constexpr int kCandidates = 8192;                // keys that share the first digit with the threshold and fit into LDS
+constexpr int kManyPositions = 65536;            // positions from which several workgroups take a sequence (60 000: 39.7 microseconds and
+                                                 // 37.7 by one; 80 000: 40 and 45; 236 000: 55 and 106)
 
 typedef float float4_any __attribute__((ext_vector_type(4), aligned(4)));
 
-// One more of `bin` for every lane of the wave that has one: lanes that agree with the first of them are added up before (weights
-// of zero, which whole rounds have, would otherwise queue at one address).
-__device__ __forceinline__ void count_bin(int* hist, bool has, int bin) {
-    const unsigned long long all = __ballot(has);
-    if (!all) return;
-    const int lane = threadIdx.x & 63, leader = __ffsll(all) - 1, common = __builtin_amdgcn_readlane(bin, leader);
-    const unsigned long long same = __ballot(has && bin == common);
-    if (lane == leader) atomicAdd(&hist[common], __popcll(same));
-    else if (has && bin != common) atomicAdd(&hist[bin], 1);
+// Bins of the counts, each four times over: lanes that meet in a bin meet in a quarter of it only.
+__device__ __forceinline__ void count_bin(int* hist, uint32_t bin) { atomicAdd(&hist[bin * 4 + (threadIdx.x & 3)], 1); }
+__device__ __forceinline__ int lanes_below(unsigned long long mask) {
+    return __builtin_amdgcn_mbcnt_hi((unsigned)(mask >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)mask, 0));
+}
+
+// Positions of a sequence: n of them; the first lo and those from hi on are kept whatever they weigh, and `need` of the others, K
+// in all.
+struct TokenRange {
+    int n, K, lo, hi, need;
+    __device__ __forceinline__ TokenRange(const SelectTokensArgs& a, int tokens) {
+        n = tokens;
+        K = min(a.budget, n);
+        lo = min(a.keep_first, n);
+        hi = n - min(a.keep_last, n - lo);
+        need = K - lo - (n - hi);
+    }
+    __device__ __forceinline__ bool all() const { return need >= hi - lo; }  // ... of the middle are kept
+    __device__ __forceinline__ bool none() const { return need <= 0; }
+    __device__ __forceinline__ bool inside(int p0) const { return p0 >= lo && p0 + kChunk <= hi; }  // the whole chunk lies in the middle
+};
+// The keys of the middle that are kept: those above `key`, and the first `equal` of those equal to it.
+struct Threshold {
+    uint32_t key;
+    int equal;
+};
+
+// First positions of the rounds, and of the end, cut off at n_pos, which is returned.  1024 threads, R_max <= 1024; a barrier at
+// its end.
+__device__ __forceinline__ int round_starts(const SelectTokensArgs& a, int b, int* start, int* wave_sum) {
+    const int r = threadIdx.x, wave = r >> 6;
+    static_assert(kMaxRounds <= kSelThreads, "a thread for every round");
+    int len = r < a.R_max ? a.seg_len[(size_t)b * a.R_max + r] : 0;
+    if (r >= a.n_rounds[b]) len = 0;
+    len = min(max(len, 0), a.n_pos);  // (64 of them add up to 2^30 at most)
+    const int incl = wave_inclusive_sum(len);
+    if ((r & 63) == 63) wave_sum[wave] = min(incl, a.n_pos);
+    __syncthreads();
+    int before = 0;
+    for (int i = 0; i < wave; ++i) before = min(before + wave_sum[i], a.n_pos);
+    if (r < a.R_max) start[r] = min(before + incl - len, a.n_pos);
+    if (r == kSelThreads - 1) start[a.R_max] = min(before + incl, a.n_pos);
+    __syncthreads();
+    return start[a.R_max];
+}
+
+// The chunks c_lo .. c_hi - 1 of n weights by a wave: f(first position of the chunk, the lane's four weights).  Past the end: zeros.
+template <typename F>
+__device__ __forceinline__ void each_chunk(const float* w, int n, int c_lo, int c_hi, F f) {
+    const int lane = threadIdx.x & 63;
+    for (int c0 = c_lo; c0 < c_hi; c0 += kChunks) {
+        float x[kChunks][4];
+#pragma unroll
+        for (int j = 0; j < kChunks; ++j) {
+            const int p = (c0 + j) * kChunk + lane * 4;
+            float4_any v = {0.f, 0.f, 0.f, 0.f};
+            if (c0 + j < c_hi) {
+                if (p + 4 <= n) {
+                    v = *reinterpret_cast<const float4_any*>(w + p);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 3; ++e)
+                        if (p + e < n) v[e] = w[p + e];
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[j][e] = v[e];
+        }
+#pragma unroll
+        for (int j = 0; j < kChunks; ++j)
+            if (c0 + j < c_hi) f((c0 + j) * kChunk, x[j]);
+    }
+}
+
+// Counts of a digit, and what is found in them.
+struct DigitCounts {
+    int hist[kBins * 4];
+    uint32_t digit;  // at which the counts, from the largest digit down, reach what is left ...
+    int left;        // ... of which so much is left then ...
+    int here;        // ... of so many candidates
+    int wave_sum[kSelWaves];
+};
+__device__ __forceinline__ void clear_counts(DigitCounts& d) {  // ends with a barrier
+    for (int i = threadIdx.x; i < kBins; i += kSelThreads) *reinterpret_cast<int4*>(&d.hist[4 * i]) = make_int4(0, 0, 0, 0);
+    __syncthreads();
+}
+__device__ __forceinline__ int count_of(const DigitCounts& d, int bin) {
+    const int4 four = *reinterpret_cast<const int4*>(&d.hist[bin * 4]);
+    return four.x + four.y + four.z + four.w;
+}
+// `count`: thread t's counts of the digits top - N t, top - N t - 1, ... (N a thread, top the largest digit).  Ends with a barrier.
+template <int N>
+__device__ __forceinline__ void find_digit(DigitCounts& d, const int (&count)[N], int left) {
+    const int tid = threadIdx.x, wave = tid >> 6;
+    int mine = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) mine += count[i];
+    const int incl = wave_inclusive_sum(mine);
+    if ((tid & 63) == 63) d.wave_sum[wave] = incl;
+    __syncthreads();
+    int taken = incl - mine;
+    for (int i = 0; i < kSelWaves; ++i) taken += i < wave ? d.wave_sum[i] : 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        if (taken < left && taken + count[i] >= left) {  // one digit of one thread
+            d.digit = (uint32_t)(kSelThreads * N - 1 - N * tid - i);
+            d.left = left - taken;
+            d.here = count[i];
+        }
+        taken += count[i];
+    }
+    __syncthreads();
+}
+template <int BITS>
+__device__ __forceinline__ void find_digit(DigitCounts& d, int left) {
+    constexpr int N = (1 << BITS) / kSelThreads;
+    int count[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) count[i] = count_of(d, kSelThreads * N - 1 - N * (int)threadIdx.x - i);
+    find_digit(d, count, left);
+}
+constexpr int kShift1 = 32 - kDigit, kShift2 = kShift1 - kDigit;  // of the first and the second digit; the third has kShift2 bits
+
+// Adds the chunks' positions of the middle to the counts of their first (second, third) digit, if they share those before with
+// `key`.  No barrier.
+template <int LEVEL>
+__device__ __forceinline__ void count_digit(DigitCounts& d, const TokenRange& range, const float* w, int c_lo, int c_hi, uint32_t key) {
+    const int lane = threadIdx.x & 63;
+    constexpr int kAbove = LEVEL == 1 ? 31 : LEVEL == 2 ? kShift1 : kShift2, kShift = LEVEL == 1 ? kShift1 : LEVEL == 2 ? kShift2 : 0;
+    constexpr uint32_t kMask = LEVEL == 3 ? (1u << kShift2) - 1 : kBins - 1;
+    int zeros = 0;  // weights of zero, which whole rounds have and which would queue at one address, are counted by the wave
+    each_chunk(w, range.n, c_lo, c_hi, [&](int p0, const float (&x)[4]) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int p = p0 + lane * 4 + e;
+            const uint32_t k = weight_key(x[e]);
+            const bool counts = (range.inside(p0) || (p >= range.lo && p < range.hi)) && (LEVEL == 1 || k >> kAbove == key >> kAbove);
+            zeros += __popcll(__ballot(counts && x[e] == 0.f));
+            if (counts && x[e] != 0.f) count_bin(d.hist, k >> kShift & kMask);
+        }
+    });
+    if (lane == 0 && zeros > 0) atomicAdd(&d.hist[(0x80000000u >> kShift & kMask) * 4], zeros);
+}
+
+// Writes the kept positions of the wave's chunks: kept for certain before them `sure`, with the threshold's key `ties`.
+// below(round, kept positions below its start) for the rounds that start in the chunks; keep(place, position, weight).
+// 0: dropped, 1: kept, 2: kept if it is among the first `equal` of its kind
+__device__ __forceinline__ int fate(const TokenRange& range, const Threshold& t, int p0, int p, float x) {
+    const uint32_t key = weight_key(x);
+    const int of_middle = range.all() ? 1 : range.none() ? 0 : key > t.key ? 1 : key == t.key ? 2 : 0;
+    return range.inside(p0) ? of_middle : p >= range.n ? 0 : p < range.lo || p >= range.hi ? 1 : of_middle;
+}
+template <typename Below, typename Keep>
+__device__ __forceinline__ void write_kept(const TokenRange& range, const Threshold& t, const float* w, int c_lo, int c_hi, int sure, int ties,
+                                           const int* start, int R, Below below, Keep keep) {
+    const int lane = threadIdx.x & 63;
+    int at = sure + min(ties, t.equal);
+    // the round whose start comes next: the first that starts at or behind these chunks
+    int round = 0;
+    for (int r0 = 0; r0 <= R; r0 += 64) round += __popcll(__ballot(r0 + lane <= R && start[min(r0 + lane, R)] < c_lo * kChunk));
+    each_chunk(w, range.n, c_lo, c_hi, [&](int p0, const float (&x)[4]) {
+        // positions in order: lane by lane, four each
+        unsigned long long kept[4], maybe[4];
+        int f[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            f[e] = fate(range, t, p0, p0 + lane * 4 + e, x[e]);
+            maybe[e] = __ballot(f[e] == 2);
+        }
+        bool mine[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) mine[e] = f[e] == 1;
+        if (maybe[0] | maybe[1] | maybe[2] | maybe[3]) {
+            int tie = ties;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) tie += lanes_below(maybe[e]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                mine[e] |= f[e] == 2 && tie < t.equal;
+                tie += f[e] == 2;
+            }
+        }
+        int j = at;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            kept[e] = __ballot(mine[e]);
+            j += lanes_below(kept[e]);
+        }
+        while (round <= R && start[round] < p0 + kChunk) {
+            const int in = start[round] - p0, in_lane = in >> 2, in_e = in & 3;
+            int under = at;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) under += __popcll(kept[e] & ((1ull << in_lane) - 1)) + (e < in_e && (kept[e] >> in_lane & 1));
+            if (lane == 0) below(round, under);
+            ++round;
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (mine[e]) keep(j++, p0 + lane * 4 + e, x[e]);
+            at += __popcll(kept[e]);
+            ties += __popcll(maybe[e]);
+        }
+    });
+}
+
+// Lengths and places of the rounds from the kept positions below their starts (below[R_max]: K), by the first wave.
+template <typename Below>
+__device__ __forceinline__ void write_rounds(const SelectTokensArgs& a, int b, int K, Below below) {
+    const int lane = threadIdx.x & 63;
+    long long off = (long long)b * a.stride;
+    for (int r0 = 0; r0 < a.R_max; r0 += 64) {
+        const int r = r0 + lane, len = r < a.R_max ? below(r + 1) - below(r) : 0;
+        const int blocks = (len + 15) / 16, incl = wave_inclusive_sum(blocks);
+        if (r < a.R_max) {
+            a.kept_len[(size_t)b * a.R_max + r] = len;
+            if (a.kept_off) a.kept_off[(size_t)b * a.R_max + r] = off + (long long)(incl - blocks) * a.unit;
+        }
+        off += (long long)__builtin_amdgcn_readlane(incl, 63) * a.unit;
+    }
+    if (lane == 0) a.n_kept[b] = K;
+}
+
+// n of `value` from `p` on, by the threads `tid` of `threads`: four at a time, and what is left of them.
+template <typename T>
+__device__ __forceinline__ void fill(T* p, int n, T value, int tid, int threads) {
+    typedef T four_t __attribute__((ext_vector_type(4), aligned(4)));
+    for (int j = tid; j < n / 4; j += threads) *reinterpret_cast<four_t*>(p + 4 * j) = four_t{value, value, value, value};
+    if (tid < n % 4) p[n / 4 * 4 + tid] = value;
 }
 
 // One workgroup per sequence.  The `need` largest weights of the middle (what is neither among the first nor the last tokens) are
@@ -50,189 +271,94 @@ __device__ __forceinline__ void count_bin(int* hist, bool has, int bin) {
 // Every wave has a contiguous sixteenth of the positions: it knows how many of them it keeps, and writes them behind what the
 // waves before it keep.  Counts are whole numbers: their order does not matter.
 //
-// Bound by a compute unit's share of the cache bandwidth and its round trips: three passes over the weights, 2 KB a wave and
-// instruction group in flight.
+// Bound by what one compute unit does in a row: 131 000 weights take it 17 microseconds to count, 26 to sort out, 22 to write.
 __global__ __launch_bounds__(kSelThreads) void select_tokens_kernel(SelectTokensArgs a) {
-    __shared__ int s_hist[kBins];
+    __shared__ __align__(16) DigitCounts d;
     __shared__ int s_start[kMaxRounds + 1], s_below[kMaxRounds + 1];
     __shared__ int s_wave[kSelWaves][2];  // positions that are kept for certain, positions with the threshold's key
     __shared__ uint2 s_cand[kCandidates];  // key, position
-    __shared__ uint32_t s_digit;
-    __shared__ int s_left, s_count, s_total;
+    __shared__ int s_count;
     const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const float* w = a.weights + (size_t)b * a.n_pos;
-    const int n_rounds = min(max(a.n_rounds[b], 0), a.R_max);
-    // first positions of the rounds
-    if (wave == 0) {
-        int before = 0;
-        for (int r0 = 0; r0 < a.R_max; r0 += 64) {
-            const int r = r0 + lane, len = r < n_rounds ? max(a.seg_len[(size_t)b * a.R_max + r], 0) : 0;
-            const int incl = wave_inclusive_sum(len);
-            if (r < a.R_max) s_start[r] = min(before + incl - len, a.n_pos);
-            before = min(before + __builtin_amdgcn_readlane(incl, 63), a.n_pos);
-        }
-        if (lane == 0) s_start[a.R_max] = s_total = before;
-    }
-    for (int i = tid; i < kBins; i += kSelThreads) s_hist[i] = 0;
-    if (tid < kSelWaves) s_wave[tid][0] = s_wave[tid][1] = 0;
     if (tid == 0) s_count = 0;
+    for (int i = tid; i < kBins; i += kSelThreads) *reinterpret_cast<int4*>(&d.hist[4 * i]) = make_int4(0, 0, 0, 0);
+    const TokenRange range(a, round_starts(a, b, s_start, s_wave[0]));
+    if (tid < kSelWaves) s_wave[tid][0] = s_wave[tid][1] = 0;
     __syncthreads();
-    const int n = s_total, K = min(a.budget, n);
-    const int first = min(a.keep_first, n), last = min(a.keep_last, n - first);
-    const int lo = first, hi = n - last, need = K - first - last;  // of the positions lo .. hi - 1
-
-    // The wave's positions, kChunk at a time: f(first position of the chunk, the lane's four weights).  Past the end: zeros.
-    const int chunks = (n + kChunk - 1) / kChunk, c_lo = chunks * wave / kSelWaves, c_hi = chunks * (wave + 1) / kSelWaves;
-    auto each_chunk = [&](auto f) {
-        for (int c0 = c_lo; c0 < c_hi; c0 += kChunks) {
-            float x[kChunks][4];
-#pragma unroll
-            for (int j = 0; j < kChunks; ++j) {
-                const int p = (c0 + j) * kChunk + lane * 4;
-                float4_any v = {0.f, 0.f, 0.f, 0.f};
-                if (c0 + j < c_hi) {
-                    if (p + 4 <= n) {
-                        v = *reinterpret_cast<const float4_any*>(w + p);
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 3; ++e)
-                            if (p + e < n) v[e] = w[p + e];
-                    }
-                }
-#pragma unroll
-                for (int e = 0; e < 4; ++e) x[j][e] = v[e];
-            }
-#pragma unroll
-            for (int j = 0; j < kChunks; ++j)
-                if (c0 + j < c_hi) f((c0 + j) * kChunk, x[j]);
-        }
-    };
-    // The digit at which the counts, from the largest one down, reach `left`; what is left of it then, and the candidates there.
-    auto find_digit = [&](int bits, int left) {
-        if (wave == 0) {
-            int taken = 0;
-            for (int i0 = (1 << bits) - 64; i0 >= 0; i0 -= 64) {
-                const int bin = i0 + 63 - lane, c = s_hist[bin], incl = wave_inclusive_sum(c);
-                const unsigned long long reached = __ballot(taken + incl >= left);
-                if (reached) {
-                    if (lane == __ffsll(reached) - 1) {
-                        s_digit = (uint32_t)bin;
-                        s_left = left - (taken + incl - c);
-                        s_total = c;
-                    }
-                    break;
-                }
-                taken += __builtin_amdgcn_readlane(incl, 63);
-            }
-        }
-        __syncthreads();
-    };
-    auto clear_bins = [&] {
-        for (int i = tid; i < kBins; i += kSelThreads) s_hist[i] = 0;
-        __syncthreads();
-    };
-
-    uint32_t threshold = 0;  // keys above it are kept, and the first `equal` of those equal to it
-    int equal = 0;
-    const bool all = need >= hi - lo, none = need <= 0;
+    const int chunks = (range.n + kChunk - 1) / kChunk, c_lo = chunks * wave / kSelWaves, c_hi = chunks * (wave + 1) / kSelWaves;
+    Threshold t = {0, 0};
     bool counted = false;  // s_wave is complete
-    if (!all && !none) {
-        constexpr int kShift1 = 32 - kDigit, kShift2 = kShift1 - kDigit;
-        each_chunk([&](int p0, const float (&x)[4]) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int p = p0 + lane * 4 + e;
-                count_bin(s_hist, p >= lo && p < hi, weight_key(x[e]) >> kShift1);
-            }
-        });
+    if (!range.all() && !range.none()) {
+        count_digit<1>(d, range, w, c_lo, c_hi, 0);
         __syncthreads();
-        find_digit(kDigit, need);
-        const uint32_t digit1 = s_digit;
-        threshold = digit1 << kShift1;
-        int left = s_left;
-        const bool in_lds = s_total <= kCandidates;
-        clear_bins();
+        find_digit<kDigit>(d, range.need);
+        const uint32_t digit1 = d.digit;
+        t.key = digit1 << kShift1;
+        int left = d.left;
+        const bool in_lds = d.here <= kCandidates;
+        clear_counts(d);
         if (in_lds) {
             int sure = 0;
-            each_chunk([&](int p0, const float (&x)[4]) {
+            each_chunk(w, range.n, c_lo, c_hi, [&](int p0, const float (&x)[4]) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int p = p0 + lane * 4 + e;
                     const uint32_t key = weight_key(x[e]), digit = key >> kShift1;
-                    const bool middle = p >= lo && p < hi;
-                    sure += __popcll(__ballot(p < n && (!middle || digit > digit1)));
+                    const bool middle = range.inside(p0) || (p >= range.lo && p < range.hi);
+                    sure += __popcll(__ballot(middle ? digit > digit1 : p < range.n));
                     const unsigned long long take = __ballot(middle && digit == digit1);
-                    if (!take) continue;
-                    int at = 0;
-                    if (lane == 0) at = atomicAdd(&s_count, __popcll(take));
-                    at = __builtin_amdgcn_readfirstlane(at) + __popcll(take & ((1ull << lane) - 1));
-                    if (take >> lane & 1) s_cand[at] = make_uint2(key, (uint32_t)p);
+                    if (take) {  // into the list, in any order
+                        int at = 0;
+                        if (lane == 0) at = atomicAdd(&s_count, __popcll(take));
+                        at = __builtin_amdgcn_readfirstlane(at) + lanes_below(take);
+                        if (middle && digit == digit1) s_cand[at] = make_uint2(key, (uint32_t)p);
+                    }
                 }
             });
             if (lane == 0) s_wave[wave][0] = sure;
             __syncthreads();
             const int n_cand = s_count;
-            for (int i = tid; i < n_cand; i += kSelThreads) atomicAdd(&s_hist[s_cand[i].x >> kShift2 & (kBins - 1)], 1);
+            for (int i = tid; i < n_cand; i += kSelThreads) count_bin(d.hist, s_cand[i].x >> kShift2 & (kBins - 1));
             __syncthreads();
-            find_digit(kDigit, left);
-            threshold |= s_digit << kShift2;
-            left = s_left;
-            clear_bins();
+            find_digit<kDigit>(d, left);
+            t.key |= d.digit << kShift2;
+            left = d.left;
+            clear_counts(d);
             for (int i = tid; i < n_cand; i += kSelThreads)
-                if (s_cand[i].x >> kShift2 == threshold >> kShift2) atomicAdd(&s_hist[s_cand[i].x & ((1 << kShift2) - 1)], 1);
+                if (s_cand[i].x >> kShift2 == t.key >> kShift2) count_bin(d.hist, s_cand[i].x & ((1 << kShift2) - 1));
             __syncthreads();
-            find_digit(kShift2, left);
-            threshold |= s_digit;
-            equal = s_left;
+            find_digit<kShift2>(d, left);
+            t.key |= d.digit;
+            t.equal = d.left;
             for (int i = tid; i < n_cand; i += kSelThreads) {
-                if (s_cand[i].x < threshold) continue;
+                if (s_cand[i].x < t.key) continue;
                 // the wave whose positions these are: the last one that begins at or before the chunk
                 const int c = (int)s_cand[i].y / kChunk;
                 int owner = (int)(((long long)c * kSelWaves) / chunks);
                 while (owner + 1 < kSelWaves && chunks * (owner + 1) / kSelWaves <= c) ++owner;
-                atomicAdd(&s_wave[owner][s_cand[i].x == threshold], 1);
+                atomicAdd(&s_wave[owner][s_cand[i].x == t.key], 1);
             }
             counted = true;
         } else {
-            each_chunk([&](int p0, const float (&x)[4]) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int p = p0 + lane * 4 + e;
-                    const uint32_t key = weight_key(x[e]);
-                    count_bin(s_hist, p >= lo && p < hi && key >> kShift1 == digit1, key >> kShift2 & (kBins - 1));
-                }
-            });
+            count_digit<2>(d, range, w, c_lo, c_hi, t.key);
             __syncthreads();
-            find_digit(kDigit, left);
-            threshold |= s_digit << kShift2;
-            left = s_left;
-            clear_bins();
-            each_chunk([&](int p0, const float (&x)[4]) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int p = p0 + lane * 4 + e;
-                    const uint32_t key = weight_key(x[e]);
-                    count_bin(s_hist, p >= lo && p < hi && key >> kShift2 == threshold >> kShift2, key & ((1 << kShift2) - 1));
-                }
-            });
+            find_digit<kDigit>(d, left);
+            t.key |= d.digit << kShift2;
+            left = d.left;
+            clear_counts(d);
+            count_digit<3>(d, range, w, c_lo, c_hi, t.key);
             __syncthreads();
-            find_digit(kShift2, left);
-            threshold |= s_digit;
-            equal = s_left;
+            find_digit<kShift2>(d, left);
+            t.key |= d.digit;
+            t.equal = d.left;
         }
     }
-    // 0: dropped, 1: kept, 2: kept if it is among the first `equal` of its kind
-    auto fate = [&](int p, float x) {
-        const uint32_t key = weight_key(x);
-        const int of_middle = all ? 1 : none ? 0 : key > threshold ? 1 : key == threshold ? 2 : 0;
-        return p >= n ? 0 : p < lo || p >= hi ? 1 : of_middle;
-    };
     if (!counted) {
         int n_sure = 0, n_equal = 0;
-        each_chunk([&](int p0, const float (&x)[4]) {
+        each_chunk(w, range.n, c_lo, c_hi, [&](int p0, const float (&x)[4]) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const int f = fate(p0 + lane * 4 + e, x[e]);
+                const int f = fate(range, t, p0, p0 + lane * 4 + e, x[e]);
                 n_sure += __popcll(__ballot(f == 1));
                 n_equal += __popcll(__ballot(f == 2));
             }
@@ -243,78 +369,196 @@ __global__ __launch_bounds__(kSelThreads) void select_tokens_kernel(SelectTokens
         }
     }
     __syncthreads();
-    int at = 0, equal_before = 0;
+    int sure = 0, ties = 0;
     for (int i = 0; i < wave; ++i) {
-        at += s_wave[i][0];
-        equal_before += s_wave[i][1];
+        sure += s_wave[i][0];
+        ties += s_wave[i][1];
     }
-    at += min(equal_before, equal);
     int32_t* idx = a.kept_idx + (size_t)b * a.budget;
     float* left_over = a.kept_weights ? a.kept_weights + (size_t)b * a.n_pos : nullptr;
-    // the round whose start comes next: the first that starts at or behind this wave's part (the first wave: round 0)
-    int round = 0;
-    for (int r0 = 0; r0 <= a.R_max; r0 += 64)
-        round += __popcll(__ballot(r0 + lane <= a.R_max && s_start[min(r0 + lane, a.R_max)] < c_lo * kChunk));
-    const unsigned long long below_lane = (1ull << lane) - 1;
-    each_chunk([&](int p0, const float (&x)[4]) {
-        // positions in order: lane by lane, four each
-        unsigned long long kept[4], maybe[4];
-        int f[4], eq = 0;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            f[e] = fate(p0 + lane * 4 + e, x[e]);
-            maybe[e] = __ballot(f[e] == 2);
-            eq += __popcll(maybe[e] & below_lane);
-        }
-        eq += equal_before;
-        int j = at;
-        bool mine[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            mine[e] = f[e] == 1 || (f[e] == 2 && eq < equal);
-            eq += f[e] == 2;
-            kept[e] = __ballot(mine[e]);
-            j += __popcll(kept[e] & below_lane);
-        }
-        while (round <= a.R_max && s_start[round] < p0 + kChunk) {
-            const int in = s_start[round] - p0, in_lane = in >> 2, in_e = in & 3;
-            int below = at;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) below += __popcll(kept[e] & ((1ull << in_lane) - 1)) + (e < in_e && (kept[e] >> in_lane & 1));
-            if (lane == 0) s_below[round] = below;
-            ++round;
-        }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            if (mine[e]) {
-                idx[j] = p0 + lane * 4 + e;
-                if (left_over) left_over[j] = x[e];
-                ++j;
-            }
-            at += __popcll(kept[e]);
-            equal_before += __popcll(maybe[e]);
-        }
-    });
-    for (int j = K + tid; j < a.budget; j += kSelThreads) idx[j] = -1;
-    if (left_over)
-        for (int j = K + tid; j < a.n_pos; j += kSelThreads) left_over[j] = 0.f;
+    write_kept(range, t, w, c_lo, c_hi, sure, ties, s_start, a.R_max, [&](int r, int under) { s_below[r] = under; },
+               [&](int j, int p, float x) {
+                   idx[j] = p;
+                   if (left_over) left_over[j] = x;
+               });
+    fill(idx + range.K, a.budget - range.K, (int32_t)-1, tid, kSelThreads);
+    if (left_over) fill(left_over + range.K, a.n_pos - range.K, 0.f, tid, kSelThreads);
     // starts behind the last chunk (and all of them, if there are no tokens): everything kept lies below
     for (int r = tid; r <= a.R_max; r += kSelThreads)
-        if (s_start[r] >= chunks * kChunk) s_below[r] = K;
+        if (s_start[r] >= chunks * kChunk) s_below[r] = range.K;
     __syncthreads();
-    if (wave == 0) {
-        long long off = (long long)b * a.stride;
-        for (int r0 = 0; r0 < a.R_max; r0 += 64) {
-            const int r = r0 + lane, len = r < a.R_max ? s_below[r + 1] - s_below[r] : 0;
-            const int blocks = (len + 15) / 16, incl = wave_inclusive_sum(blocks);
-            if (r < a.R_max) {
-                a.kept_len[(size_t)b * a.R_max + r] = len;
-                if (a.kept_off) a.kept_off[(size_t)b * a.R_max + r] = off + (long long)(incl - blocks) * a.unit;
-            }
-            off += (long long)__builtin_amdgcn_readlane(incl, 63) * a.unit;
-        }
-        if (lane == 0) a.n_kept[b] = K;
+    if (wave == 0) write_rounds(a, b, range.K, [&](int r) { return s_below[r]; });
+}
+
+// ---- the same by several workgroups per sequence ------------------------------------------------------------------------------
+// Every workgroup has a part of the positions.  Three launches count the digits, each of them adding up what the one before
+// counted in all parts; one writes the kept positions, every part behind what the parts before it keep; the last one writes
+// the rounds and the weights.  Until then the counts lie where those weights will: kept_weights holds them (5120 numbers a part
+// of 16384 positions or more, from two parts on).
+constexpr int kPartPositions = 16384;  // (with 8192: 16 dialogues of 131 000 tokens 71 microseconds instead of 60; with 32768: 74)
+struct SelectParts {
+    int n, chunks;  // parts; chunks of a part
+    __host__ __device__ static SelectParts of(int n_pos) {
+        SelectParts s;
+        s.chunks = kPartPositions / kChunk * ((n_pos + 64 * kPartPositions - 1) / (64 * kPartPositions));  // 64 parts at most: each adds up the counts of all
+        s.n = (n_pos + s.chunks * kChunk - 1) / (s.chunks * kChunk);
+        return s;
     }
+    __device__ int used(int positions) const { return (positions + chunks * kChunk - 1) / (chunks * kChunk); }  // parts with positions
+    __host__ __device__ size_t scratch() const { return (size_t)n * (2 * kBins + (1 << kShift2) + 2) + 4; }  // numbers
+};
+struct SelectScratch {
+    int *count1, *count2, *count3;  // [parts][bins]
+    int* found;                     // digit and what is left, of the first and the second level
+    int* above;                     // [parts][2]: positions of the part above the first (second) digit
+    __device__ __forceinline__ SelectScratch(const SelectTokensArgs& a, int b, int parts) {
+        count1 = reinterpret_cast<int*>(a.kept_weights + (size_t)b * a.n_pos);
+        count2 = count1 + (size_t)parts * kBins;
+        count3 = count2 + (size_t)parts * kBins;
+        above = count3 + ((size_t)parts << kShift2);
+        found = above + 2 * parts;
+    }
+};
+
+// Adds up a level's counts of all parts and finds the digit.  `mine`: the counts of this part, `before`: of the parts before it, of
+// the digits that find_digit gives the thread.
+template <int N>
+__device__ __forceinline__ int thread_digit(int i) { return kSelThreads * N - 1 - N * (int)threadIdx.x - i; }
+template <int N>
+__device__ __forceinline__ void add_parts(DigitCounts& d, const int* counts, int parts, int part, int left, int (&mine)[N], int (&before)[N]) {
+    int sum[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) sum[i] = mine[i] = before[i] = 0;
+    for (int p0 = 0; p0 < parts; p0 += 16) {
+        int c[16][N];
+#pragma unroll
+        for (int p = 0; p < 16; ++p)
+#pragma unroll
+            for (int i = 0; i < N; ++i) c[p][i] = p0 + p < parts ? counts[(size_t)(p0 + p) * (kSelThreads * N) + thread_digit<N>(i)] : 0;
+#pragma unroll
+        for (int p = 0; p < 16; ++p)
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                sum[i] += c[p][i];
+                mine[i] += p0 + p == part ? c[p][i] : 0;
+                before[i] += p0 + p < part ? c[p][i] : 0;
+            }
+    }
+    find_digit(d, sum, left);
+}
+// Sum over the threads, in every thread; two barriers.
+__device__ __forceinline__ int block_sum(int v, int* wave_sum) {
+    v = wave_inclusive_sum(v);
+    if ((threadIdx.x & 63) == 63) wave_sum[threadIdx.x >> 6] = v;
+    __syncthreads();
+    int sum = 0;
+    for (int i = 0; i < kSelWaves; ++i) sum += wave_sum[i];
+    __syncthreads();
+    return sum;
+}
+
+// grid (parts, B)
+template <int LEVEL>
+__global__ __launch_bounds__(kSelThreads) void select_count_kernel(SelectTokensArgs a, SelectParts parts) {
+    __shared__ __align__(16) DigitCounts d;
+    __shared__ int s_start[kMaxRounds + 1], s_wave[kSelWaves];
+    const int part = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const TokenRange range(a, round_starts(a, b, s_start, s_wave));
+    const int used = parts.used(range.n);
+    if (part >= used) return;
+    const SelectScratch at(a, b, parts.n);
+    uint32_t key = 0;
+    if constexpr (LEVEL > 1) {
+        const uint32_t digit1 = LEVEL == 3 ? (uint32_t)at.found[0] : 0;
+        const int left = LEVEL == 3 ? at.found[1] : range.need;
+        int mine[2], before[2];
+        add_parts(d, LEVEL == 2 ? at.count1 : at.count2, used, part, left, mine, before);
+        const uint32_t digit = d.digit;
+        if (part == 0 && tid == 0) {
+            at.found[2 * (LEVEL - 2)] = (int)digit;
+            at.found[2 * (LEVEL - 2) + 1] = d.left;
+        }
+        key = LEVEL == 2 ? digit << kShift1 : digit1 << kShift1 | digit << kShift2;
+        const int above = block_sum(((uint32_t)thread_digit<2>(0) > digit ? mine[0] : 0) + ((uint32_t)thread_digit<2>(1) > digit ? mine[1] : 0), s_wave);
+        if (tid == 0) at.above[2 * part + LEVEL - 2] = above;
+    }
+    clear_counts(d);
+    const int c0 = part * parts.chunks, chunks = max(min((range.n + kChunk - 1) / kChunk - c0, parts.chunks), 0);
+    count_digit<LEVEL>(d, range, a.weights + (size_t)b * a.n_pos, c0 + chunks * wave / kSelWaves, c0 + chunks * (wave + 1) / kSelWaves, key);
+    __syncthreads();
+    constexpr int kCounts = LEVEL == 3 ? 1 << kShift2 : kBins;
+    int* out = (LEVEL == 1 ? at.count1 : LEVEL == 2 ? at.count2 : at.count3) + (size_t)part * kCounts;
+    for (int i = tid; i < kCounts; i += kSelThreads) out[i] = count_of(d, i);
+}
+
+// grid (parts, B): the kept positions, and in kept_len how many of them lie below the rounds' starts
+__global__ __launch_bounds__(kSelThreads) void select_write_kernel(SelectTokensArgs a, SelectParts parts) {
+    __shared__ __align__(16) DigitCounts d;
+    __shared__ int s_start[kMaxRounds + 1], s_wave[kSelWaves], s_sure[kSelWaves], s_ties[kSelWaves];
+    const int part = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const TokenRange range(a, round_starts(a, b, s_start, s_wave));
+    const SelectScratch at(a, b, parts.n);
+    const float* w = a.weights + (size_t)b * a.n_pos;
+    int32_t* idx = a.kept_idx + (size_t)b * a.budget;
+    fill(idx + range.K, a.budget - range.K, (int32_t)-1, part * kSelThreads + tid, parts.n * kSelThreads);
+    int32_t* below = a.kept_len + (size_t)b * a.R_max;
+    if (part == 0)  // starts behind the last chunk: everything kept lies below
+        for (int r = tid; r < a.R_max; r += kSelThreads)
+            if (s_start[r] >= (range.n + kChunk - 1) / kChunk * kChunk) below[r] = range.K;
+    const int used = parts.used(range.n);
+    if (part >= used) return;
+    int mine[1], before[1];
+    add_parts(d, at.count3, used, part, at.found[3], mine, before);
+    const uint32_t digit3 = d.digit;
+    const Threshold t = {(uint32_t)at.found[0] << kShift1 | (uint32_t)at.found[2] << kShift2 | digit3, d.left};
+    // what the parts before this one keep
+    const int c0 = part * parts.chunks, chunks = max(min((range.n + kChunk - 1) / kChunk - c0, parts.chunks), 0), p0 = min(c0 * kChunk, range.n);
+    const int forced = min(range.lo, p0) + max(p0 - range.hi, 0);
+    int sure = block_sum(((uint32_t)thread_digit<1>(0) > digit3 ? before[0] : 0) + (tid < part ? at.above[2 * tid] + at.above[2 * tid + 1] : 0), s_wave) + forced;
+    int ties = block_sum((uint32_t)thread_digit<1>(0) == digit3 ? before[0] : 0, s_wave);
+    if (range.all()) sure = p0, ties = 0;
+    else if (range.none()) sure = forced, ties = 0;
+    const int c_lo = c0 + chunks * wave / kSelWaves, c_hi = c0 + chunks * (wave + 1) / kSelWaves;
+    int n_sure = 0, n_ties = 0;
+    each_chunk(w, range.n, c_lo, c_hi, [&](int p, const float (&x)[4]) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int f = fate(range, t, p, p + lane * 4 + e, x[e]);
+            n_sure += __popcll(__ballot(f == 1));
+            n_ties += __popcll(__ballot(f == 2));
+        }
+    });
+    if (lane == 0) {
+        s_sure[wave] = n_sure;
+        s_ties[wave] = n_ties;
+    }
+    __syncthreads();
+    for (int i = 0; i < wave; ++i) {
+        sure += s_sure[i];
+        ties += s_ties[i];
+    }
+    write_kept(range, t, w, c_lo, c_hi, sure, ties, s_start, a.R_max, [&](int r, int under) { if (r < a.R_max) below[r] = under; },
+               [&](int j, int p, float) { idx[j] = p; });
+}
+
+// grid (pieces of kFinish weights, B)
+constexpr int kFinish = 4 * kSelThreads;
+__global__ __launch_bounds__(kSelThreads) void select_finish_kernel(SelectTokensArgs a) {
+    __shared__ int s_start[kMaxRounds + 1], s_wave[kSelWaves], s_below[kMaxRounds + 1];
+    const int part = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
+    const TokenRange range(a, round_starts(a, b, s_start, s_wave));
+    const float* w = a.weights + (size_t)b * a.n_pos;
+    const int32_t* idx = a.kept_idx + (size_t)b * a.budget;
+    float* out = a.kept_weights + (size_t)b * a.n_pos;
+    const int first = part * kFinish, last = min(first + kFinish, a.n_pos), kept = min(max(range.K - first, 0), last - first);
+#pragma unroll
+    for (int i = 0; i < kFinish / kSelThreads; ++i)
+        if (const int j = i * kSelThreads + tid; j < kept) out[first + j] = w[idx[first + j]];
+    fill(out + first + kept, last - first - kept, 0.f, tid, kSelThreads);
+    if (part != 0) return;
+    for (int r = tid; r <= a.R_max; r += kSelThreads) s_below[r] = r < a.R_max ? a.kept_len[(size_t)b * a.R_max + r] : range.K;
+    __syncthreads();
+    if (tid < 64) write_rounds(a, b, range.K, [&](int r) { return s_below[r]; });
 }
 
 // ---- the smaller cache -------------------------------------------------------------------------------------------------------
@@ -570,7 +814,18 @@ extern "C" int ra_select_tokens(ra_ctx* ctx, void* stream, const float* weights,
     a.kept_len = kept_len;
     a.kept_off = reinterpret_cast<long long*>(kept_off);
     a.kept_weights = kept_weights;
-    hipLaunchKernelGGL(select_tokens_kernel, dim3((unsigned)B), dim3(kSelThreads), 0, reinterpret_cast<hipStream_t>(stream), a);
+    hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+    const SelectParts parts = SelectParts::of(n_pos);
+    if (kept_weights != nullptr && n_pos >= kManyPositions && parts.scratch() <= (size_t)n_pos && B <= 65535) {
+        const dim3 grid((unsigned)parts.n, (unsigned)B), block(kSelThreads);
+        hipLaunchKernelGGL((select_count_kernel<1>), grid, block, 0, st, a, parts);
+        hipLaunchKernelGGL((select_count_kernel<2>), grid, block, 0, st, a, parts);
+        hipLaunchKernelGGL((select_count_kernel<3>), grid, block, 0, st, a, parts);
+        hipLaunchKernelGGL(select_write_kernel, grid, block, 0, st, a, parts);
+        hipLaunchKernelGGL(select_finish_kernel, dim3((unsigned)((n_pos + kFinish - 1) / kFinish), (unsigned)B), block, 0, st, a);
+    } else {
+        hipLaunchKernelGGL(select_tokens_kernel, dim3((unsigned)B), dim3(kSelThreads), 0, st, a);
+    }
     RA_HIP_CHECK(hipGetLastError());
     return RA_OK;
 }
