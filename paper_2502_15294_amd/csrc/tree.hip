@@ -7,6 +7,8 @@
 #include "mfma_util.hpp"
 #include "stream_kv.hpp"
 
+#include <algorithm>
+
 namespace ra {
 
 __device__ __forceinline__ floatx4_t mfma4(float a, float b, floatx4_t c) {
@@ -159,30 +161,368 @@ __global__ __launch_bounds__(256) void tree_f32_kernel(AttnArgs a, int n_rowbloc
     }
 }
 
-static int tree_attention_f32(ra_ctx* ctx, hipStream_t st, AttnArgs& a, int64_t max_tokens) {
-    const int B = a.view.B, Hkv = a.view.Hkv, D = a.view.d, n_rowblocks = (a.q_len * a.G + 63) / 64;
+// ---- bf16, 128 channels, many query rows per KV head ---------------------------------------------------------------------------
+// Arithmetic of the question kernel (S^T = K . Q^T, O^T += V^T . P, query row = lane % 16, the softmax reference of a row raised
+// only when a logit exceeds it by more than 2^16 after scaling), but the keys come in steps of four UNITS of 16 tokens, a unit
+// being what one value tile holds and never crossing a round, and the roles of the lanes are dealt out by unit:
+//   * row r of the operand K of tile h (h = 0 .. 3) is token 4 h + r % 4 of unit r / 4, so that lane group q of the product holds
+//     the logits of unit q, tokens 4 h .. 4 h + 3, and after tiles 2 m and 2 m + 1 the eight probabilities of tokens
+//     8 m .. 8 m + 7 of unit q: the P operand of the products over those tokens of all four units;
+//   * the V^T operand of lane group q is then 16 contiguous bytes of unit q's value tile.
+// A unit needs one address for its keys and one for its values.  The workgroup looks up 256 units at a time (a thread each) and
+// keeps the addresses in LDS; wave w brings the keys of a step's unit w, four instructions of four whole rows, and two channel
+// groups of the values, all with one base address a lane and constant offsets.  So the loop has no segment walk, no block-table
+// look-up and next to no address arithmetic, and one barrier per 64 tokens.  (The question kernel walks the segments in scalar
+// registers, which it has too few of, once per 32 tokens: fourteen vector instructions for every exponential, here nine; 60
+// drafted tokens of 64 heads over 32 paged dialogues of 4 900 tokens: TREE_OLD -> TREE_NEW microseconds.)
+// Units of the current round, whose values are token-major and whose keys lie Hkv rows apart, take a slower path: their values
+// are gathered by 2-byte loads.
+//
+// P goes to the matrix cores as the sum of two bf16 numbers, both rounded to the nearest: a weight is off by 2^-18 of itself at most.
+constexpr int kUnitsAhead = 256;                    // units that are looked up at a time
+constexpr int kStepUnits = 4, kStepBytes = 32768;   // 16 KB of keys, 16 KB of values
+constexpr int kTreeWaves = 2;                       // workgroups of a compute unit, waves of a SIMD
+
+struct UnitTable {
+    long long key[kUnitsAhead], value[kUnitsAhead];  // addresses of the unit's first key, and of its value tile (first value)
+    int tokens[kUnitsAhead];                         // 1 .. 16; of the current round: + 32
+    int first[kUnitsAhead];                          // first token inside its segment
+};
+
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"  // M0 is named as clobbered; the compiler sets it anew before each of its own uses
+// As load_to_lds, OFFSET bytes behind `base`.  The instruction adds its offset to the LDS address too, and takes 16 bits of M0: the
+// steps lie in the first 64 KB of LDS.
+template <int OFFSET>
+__device__ __forceinline__ void load_to_lds_at(long long base, unsigned lds) {
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off offset:%2" : : "v"(base), "s"(lds - OFFSET), "n"(OFFSET) : "memory", "m0");
+}
+#pragma clang diagnostic pop
+
+// RT: 16-row tiles of a wave (one workgroup: four waves, 64 RT rows).  grid (pieces x row blocks x KV heads x sequences)
+template <bool PAGED, int RT>
+__global__ __launch_bounds__(256, kTreeWaves) void tree_rows_kernel(AttnArgs a, int n_rowblocks) {
+    extern __shared__ __align__(16) char smem[];  // (all of the kernel's LDS: the steps come first)
+    const DevView& vw = a.view;
+    const int Hkv = vw.Hkv, G = a.G, cap = vw.R_max + 1;
+    const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, q4 = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    char* tiles = smem;  // two steps
+    UnitTable& units = *reinterpret_cast<UnitTable*>(smem + 2 * kStepBytes);
+    int* cum = reinterpret_cast<int*>(smem + 2 * kStepBytes + sizeof(UnitTable));
+    const unsigned tiles_lds = __builtin_amdgcn_readfirstlane((unsigned)(size_t)(lptr_t)tiles);
+
+    // Neighbours share keys (the row blocks of a piece, then the pieces): they go to the same die.
+    const int dies = 8, die = blockIdx.x % dies, each = gridDim.x / dies, more = gridDim.x - each * dies;
+    int item = die * each + min(die, more) + (int)blockIdx.x / dies;
+    const int rowblock = item % n_rowblocks;
+    item /= n_rowblocks;
+    const int s = item % a.S;
+    item /= a.S;
+    const int g = item % Hkv, b = item / Hkv;
+
+    const char* plan = a.plan + (size_t)b * plan_stride(cap);
+    const PlanHeader hdr = *reinterpret_cast<const PlanHeader*>(plan);
+    const long long* off_k = reinterpret_cast<const long long*>(plan + sizeof(PlanHeader));
+    const long long* off_v = off_k + cap;
+    const int* lens = reinterpret_cast<const int*>(off_v + cap);
+    for (int i = tid; i <= cap; i += 256) cum[i] = lens[cap + i];
+    const int committed = committed_tokens(a, b), drafted = drafted_tokens(a, b, committed);
+    // ---- this wave's query rows: the block's 16-row tiles are dealt out to the waves in turn ---------------------------------
+    const int rows = a.q_len * G;
+    const RowsPerToken per_token(G);
+    int node[RT];
+    bool row_ok[RT];
+    size_t rowid[RT];
+    uint4 q[RT][4];
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+        const int row = ((rowblock * RT + t) * 4 + wave) * 16 + n;
+        row_ok[t] = row < rows;
+        const int r = row_ok[t] ? row : 0;
+        node[t] = per_token.token(r);
+        rowid[t] = ((size_t)b * a.q_len + node[t]) * a.Hq + (size_t)g * G + (r - node[t] * G);
+        const uint4* qp = reinterpret_cast<const uint4*>(static_cast<const char*>(a.q) + rowid[t] * 256);
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) q[t][kk] = qp[kk * 4 + q4];
+    }
+    const int n_slots = __builtin_amdgcn_readfirstlane(hdr.n_slots), n_hist = __builtin_amdgcn_readfirstlane(hdr.n_hist);
+    const int S_eff = __builtin_amdgcn_readfirstlane(hdr.S_eff), U = __builtin_amdgcn_readfirstlane(hdr.U);
+    if (s >= S_eff) return;
+    const int u_lo = (int)(((long long)U * s) / S_eff), u_hi = (int)(((long long)U * (s + 1)) / S_eff);
+
+    floatx4_t acc[RT][8];
+    float m[RT], l[RT];
+    const float slack = 16.f / a.c;
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+        m[t] = kNegBig;
+        l[t] = 0.f;
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt) acc[t][dt] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+    }
+    // Keys: LDS row 16 h + r holds operand row r of tile h, its 16-byte chunk x at position (x + r) mod 16.  Wave w fills rows
+    // 16 h + 4 w .. + 3 (unit w), 16 lanes a row: chunk of the lane, from the row's start.
+    const unsigned key_chunk = (unsigned)((n - (4 * wave + q4)) & 15) * 16u;
+
+    // What of a step does not come by direct loads: values of units of the current round, on their way through registers.
+    struct Pending {
+        uint4 v[4];
+        bool some;
+    };
+    // Step `it` of the units looked up goes to `lds`.  Units past the last one repeat it (their tokens are masked).
+    auto load_step = [&](int it, int n_units, unsigned lds) -> Pending {
+        Pending p;
+        p.some = false;
+        p.v[0] = p.v[1] = p.v[2] = p.v[3] = make_uint4(0, 0, 0, 0);
+        const int ku = min(it * kStepUnits + wave, n_units - 1), vu = min(it * kStepUnits + q4, n_units - 1);
+        const int k_tokens = __builtin_amdgcn_readfirstlane(units.tokens[ku]), v_tokens = units.tokens[vu];
+        const long long k0 = units.key[ku], v0 = units.value[vu];
+        const unsigned kd = lds + 4 * wave * 256;
+        if (k_tokens == 16 || (PAGED && k_tokens < 32)) {  // whole rows 256 bytes apart (a block has 16 of them in any case)
+            const long long base = k0 + q4 * 256 + key_chunk;
+            load_to_lds_at<0>(base, kd);
+            load_to_lds_at<1024>(base, kd + 4096);
+            load_to_lds_at<2048>(base, kd + 8192);
+            load_to_lds_at<3072>(base, kd + 12288);
+        } else {
+            const long long stride = k_tokens >= 32 ? (long long)Hkv * 256 : 256;
+            const int last = (k_tokens & 31) - 1;
+#pragma unroll
+            for (int h = 0; h < 4; ++h) load_to_lds_at<0>(k0 + min(4 * h + q4, last) * stride + key_chunk, kd + h * 4096);
+        }
+        // values: fragment (dt, m) holds lane L's 16 bytes at (2 dt + m) * 1024 + 16 L: tokens 8 m .. + 7 of unit L / 16, channel
+        // 16 dt + L % 16; this wave: dt = 2 wave, 2 wave + 1
+        const unsigned vd = lds + 16384 + 4 * wave * 1024;
+        if (!__any(v_tokens >= 32)) {
+            const long long base = v0 + wave * 1024 + n * 32;
+            load_to_lds_at<0>(base, vd);
+            load_to_lds_at<16>(base, vd + 1024);
+            load_to_lds_at<512>(base, vd + 2048);
+            load_to_lds_at<528>(base, vd + 3072);
+        } else {
+            p.some = true;
+            const int last = (v_tokens & 31) - 1;
+#pragma unroll
+            for (int f = 0; f < 4; ++f) {
+                const int channel = (2 * wave + f / 2) * 16 + n;
+                if (v_tokens >= 32) {  // token-major: eight tokens of a channel
+                    uint32_t e[8];
+#pragma unroll
+                    for (int t = 0; t < 8; ++t)
+                        e[t] = *reinterpret_cast<const unsigned short*>(v0 + (long long)min(8 * (f & 1) + t, last) * Hkv * 256 + channel * 2);
+                    p.v[f] = make_uint4(e[0] | (e[1] << 16), e[2] | (e[3] << 16), e[4] | (e[5] << 16), e[6] | (e[7] << 16));
+                } else {
+                    p.v[f] = *reinterpret_cast<const uint4*>(v0 + channel * 32 + (f & 1) * 16);
+                }
+            }
+        }
+        return p;
+    };
+    auto consume = [&](const char* buf, int it, int n_units) {
+        const uint4* kb = reinterpret_cast<const uint4*>(buf);
+        const uint4* vb = reinterpret_cast<const uint4*>(buf + 16384);
+        const int unit = it * kStepUnits + q4, at = min(unit, n_units - 1);
+        const int tokens = units.tokens[at], first = units.first[at];
+        const int limit = unit < n_units ? tokens & 31 : 0;  // tokens of the lane's unit
+        const bool drafts = tokens >= 32 && first + kUnitTokens > committed;
+        const bool whole = __all(limit == 16 && !drafts);
+#pragma unroll
+        for (int m2 = 0; m2 < 2; ++m2) {  // tokens 8 m2 .. + 7 of every unit
+            uint4 kf[2][4];
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int kk = 0; kk < 4; ++kk) kf[h][kk] = kb[((2 * m2 + h) * 16 + n) * 16 + ((kk * 4 + q4 + n) & 15)];
+            floatx4_t sc[RT][2];
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk)  // independent chains interleaved
+#pragma unroll
+                for (int t = 0; t < RT; ++t)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+                        sc[t][h] = mfma16(kf[h][kk], q[t][kk], kk ? sc[t][h] : floatx4_t{0.f, 0.f, 0.f, 0.f});
+            if (!whole) {
+#pragma unroll
+                for (int t = 0; t < RT; ++t) {
+                    uint32_t sees = (1u << limit) - 1;
+                    if (drafts)
+                        sees &= tree_sees(a.tree_mask + ((size_t)b * a.q_len + node[t]) * a.tree_words, a.tree_words, first, committed);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (!(sees >> (8 * m2 + 4 * h + i) & 1)) sc[t][h][i] = -__builtin_inff();
+                }
+            }
+            bool raise = false;
+            float mx[RT];
+#pragma unroll
+            for (int t = 0; t < RT; ++t) {
+                mx[t] = max8(sc[t][0], sc[t][1]);
+                raise |= mx[t] > m[t] + slack;
+            }
+            if (__any(raise)) {
+#pragma unroll
+                for (int t = 0; t < RT; ++t) {
+                    const float m_new = vmax(m[t], xrow_max4(mx[t])), alpha = fast_exp2((m[t] - m_new) * a.c);
+                    l[t] *= alpha;
+#pragma unroll
+                    for (int dt = 0; dt < 8; ++dt) acc[t][dt] *= alpha;
+                    m[t] = m_new;
+                }
+            }
+            uint4 vf[8];  // shared by the row tiles
+#pragma unroll
+            for (int dt = 0; dt < 8; ++dt) vf[dt] = vb[(2 * dt + m2) * 64 + lane];
+            // row tile by row tile: the first one's products can run while the second one's logits become probabilities
+#pragma unroll
+            for (int t = 0; t < RT; ++t) {
+                const float mc = m[t] * a.c;
+                float p[8];
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) p[h * 4 + i] = fast_exp2(__builtin_fmaf(sc[t][h][i], a.c, -mc));
+                l[t] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+                const uint4 hi = make_uint4(pack_nearest(p[0], p[1]), pack_nearest(p[2], p[3]), pack_nearest(p[4], p[5]), pack_nearest(p[6], p[7]));
+                const uint4 lo = make_uint4(
+                    pack_nearest(p[0] - low_bf16(hi.x), p[1] - high_bf16(hi.x)), pack_nearest(p[2] - low_bf16(hi.y), p[3] - high_bf16(hi.y)),
+                    pack_nearest(p[4] - low_bf16(hi.z), p[5] - high_bf16(hi.z)), pack_nearest(p[6] - low_bf16(hi.w), p[7] - high_bf16(hi.w)));
+#pragma unroll
+                for (int dt = 0; dt < 8; ++dt) {
+                    acc[t][dt] = mfma16(vf[dt], hi, acc[t][dt]);
+                    acc[t][dt] = mfma16(vf[dt], lo, acc[t][dt]);
+                }
+            }
+        }
+    };
+
+    for (int c0 = u_lo; c0 < u_hi; c0 += kUnitsAhead) {
+        const int n_units = min(kUnitsAhead, u_hi - c0), n_steps = (n_units + kStepUnits - 1) / kStepUnits;
+        __syncthreads();  // the prefix is there; the units and the steps before are read
+        if (tid < n_units) {
+            const int u = c0 + tid, slot = find_slot(cum, n_slots, u), first = (u - cum[slot]) * kUnitTokens, len = lens[slot];
+            const int tokens = min(kUnitTokens, len - first);
+            long long key, value;
+            if (slot >= n_hist) {
+                const size_t row = (((size_t)b * a.cur_cap + first) * Hkv + g) * 256;
+                key = reinterpret_cast<long long>(a.cur_k) + row;
+                value = reinterpret_cast<long long>(a.cur_v) + row;
+            } else if (PAGED) {
+                const long long entry = min(max(off_k[slot] + first / 16, 0ll), (long long)vw.max_blocks - 1);
+                const size_t block = ((size_t)max(vw.block_table[(size_t)b * vw.max_blocks + entry], 0) * Hkv + g) * 4096;
+                key = reinterpret_cast<long long>(vw.k) + block;
+                value = reinterpret_cast<long long>(vw.v) + block;
+            } else {
+                key = reinterpret_cast<long long>(vw.k) + ((size_t)off_k[slot] * Hkv + (size_t)g * len + first) * 256;
+                value = reinterpret_cast<long long>(vw.v) + ((size_t)off_v[slot] * Hkv + (size_t)g * ((len + 15) & ~15) + first) * 256;
+            }
+            units.key[tid] = key;
+            units.value[tid] = value;
+            units.tokens[tid] = tokens + (slot >= n_hist ? 32 : 0);
+            units.first[tid] = first;
+        }
+        __syncthreads();
+        Pending p = load_step(0, n_units, tiles_lds);
+        for (int it = 0; it < n_steps; ++it) {
+            char* buf = tiles + (it & 1) * kStepBytes;
+            if (p.some) {
+                uint4* vd = reinterpret_cast<uint4*>(buf + 16384) + 4 * wave * 64 + lane;
+#pragma unroll
+                for (int f = 0; f < 4; ++f) vd[f * 64] = p.v[f];
+            }
+            wait_for_direct_loads();  // this wave's part of the step has landed in LDS
+            __syncthreads();
+            if (it + 1 < n_steps) p = load_step(it + 1, n_units, tiles_lds + ((it + 1) & 1) * kStepBytes);
+            consume(buf, it, n_units);
+        }
+    }
+
+    // ---- the four lane groups hold partial sums of the same rows; each wave owns its rows --------------------------------------
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+        l[t] = xrow_sum4(l[t]);
+        if (node[t] >= drafted) {  // no token of this sequence's tree: as a row that sees nothing
+            m[t] = kNegBig;
+            l[t] = 0.f;
+#pragma unroll
+            for (int dt = 0; dt < 8; ++dt) acc[t][dt] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+        }
+        if (!row_ok[t]) continue;
+        if (S_eff > 1) {
+            const size_t pr = rowid[t] * a.S + s;
+#pragma unroll
+            for (int dt = 0; dt < 8; ++dt) *reinterpret_cast<floatx4_t*>(a.part_acc + pr * 128 + dt * 16 + q4 * 4) = acc[t][dt];
+            if (q4 == 0) {
+                a.part_m[pr] = m[t];
+                a.part_l[pr] = l[t];
+            }
+        } else {
+            const float inv = l[t] > 0.f ? 1.f / l[t] : 0.f;
+#pragma unroll
+            for (int dt = 0; dt < 8; ++dt) *reinterpret_cast<floatx4_t*>(a.out + rowid[t] * 128 + dt * 16 + q4 * 4) = acc[t][dt] * inv;
+            if (a.lse && q4 == 0) a.lse[rowid[t]] = l[t] > 0.f ? __builtin_fmaf(m[t], a.scale, __builtin_logf(l[t])) : -__builtin_inff();
+        }
+    }
+}
+
+// Pieces that every sequence is cut into at most, for `items` workgroups a piece of which `at_once` run at the same time: as many
+// as those, or, if there are more items than that, the fewest pieces with which the last turn is nearly full.
+static int tree_pieces(long long items, long long at_once, int64_t max_units, int min_units) {
+    int64_t most = max_units / min_units;
+    if (most < 1) most = 1;
+    if (most > 64) most = 64;
+    if (items < at_once) return (int)std::min<int64_t>(at_once / items, most);
+    for (int S = 1; S <= 4 && S <= most; ++S) {
+        const long long turns = (items * S + at_once - 1) / at_once;
+        if (turns * at_once * 8 <= items * S * 9) return S;
+    }
+    return (int)std::min<int64_t>(4, most);
+}
+
+constexpr int kTreeRows = 17;  // query rows per KV head from which the waves share keys and values through LDS
+
+static int tree_attention(ra_ctx* ctx, hipStream_t st, AttnArgs& a, bool bf16) {
+    const int B = a.view.B, Hkv = a.view.Hkv, D = a.view.d, rows_total = a.q_len * a.G;
+    const int row_tiles = bf16 && rows_total > 64 ? 2 : 1;  // of a wave
+    const int n_rowblocks = (rows_total + 64 * row_tiles - 1) / (64 * row_tiles);
     const long long inner = (long long)Hkv * n_rowblocks;
-    RA_REQUIRE(inner <= 65535 && B <= kMaxBatch, RA_ERR_UNSUPPORTED, "tree: %lld blocks of rows or %d sequences are too many", inner, B);
-    const size_t rows = (size_t)B * a.q_len * a.Hq;
-    a.S = decode_splits(ctx->num_cu, B, (int)inner, max_tokens);
-    const AttnWorkspace w = attn_workspace(rows, a.S, D, B, a.view.R_max);
+    RA_REQUIRE(B <= kMaxBatch, RA_ERR_UNSUPPORTED, "tree: batch %d exceeds %d", B, kMaxBatch);
+    RA_REQUIRE(inner <= 65535 && inner * B * 64 < (1ll << 31), RA_ERR_UNSUPPORTED, "tree: %lld blocks of rows are too many", inner);
+    const int64_t max_tokens = a.max_tokens + a.cur_cap;
+    RA_REQUIRE(max_tokens < (int64_t)1 << 30, RA_ERR_UNSUPPORTED, "tree: max_tokens too large");
+    const size_t rows = (size_t)B * rows_total * Hkv;
+    a.min_units = 8;  // 128 tokens
+    a.S = bf16 ? tree_pieces(inner * B, (long long)kTreeWaves * ctx->num_cu, max_tokens / kUnitTokens, a.min_units)
+               : decode_splits(ctx->num_cu, B, (int)inner, max_tokens);
+    AttnWorkspace w = attn_workspace(rows, a.S, D, B, a.view.R_max);
+    while (a.S > 1 && w.total > ctx->ws.bytes) w = attn_workspace(rows, --a.S, D, B, a.view.R_max);
     RA_REQUIRE(ctx->ws.base != nullptr && ctx->ws.bytes >= w.total, RA_ERR_WORKSPACE,
                "tree: workspace has %zu bytes, this call needs %zu", ctx->ws.bytes, w.total);
-    a.min_units = attn_min_units();
     a.part_acc = reinterpret_cast<float*>(ctx->ws.base + w.acc_off);
     a.part_m = reinterpret_cast<float*>(ctx->ws.base + w.m_off);
     a.part_l = reinterpret_cast<float*>(ctx->ws.base + w.l_off);
     a.n_parts = reinterpret_cast<int*>(ctx->ws.base);
     a.plan = ctx->ws.base + w.plan_off;
     launch_plan(a, kUnitTokens, st);
-    const dim3 grid((unsigned)a.S, (unsigned)inner, (unsigned)B);
-    const size_t smem = align_up(SlotTable::bytes(a.view.R_max + 1), 16) + (16 * (D + 4) + D * 20) * sizeof(float);
     const bool paged = a.view.block_size != 0;
     KernelTimer timer(ctx, st);
-    if (D == 128 && paged) RA_LAUNCH_TIMED((tree_f32_kernel<128, true>), grid, dim3(256), smem, st, a, n_rowblocks);
-    else if (D == 128) RA_LAUNCH_TIMED((tree_f32_kernel<128, false>), grid, dim3(256), smem, st, a, n_rowblocks);
-    else if (paged) RA_LAUNCH_TIMED((tree_f32_kernel<64, true>), grid, dim3(256), smem, st, a, n_rowblocks);
-    else RA_LAUNCH_TIMED((tree_f32_kernel<64, false>), grid, dim3(256), smem, st, a, n_rowblocks);
+    if (bf16) {
+        const dim3 grid((unsigned)(a.S * inner * B));
+        const size_t smem = 2 * kStepBytes + sizeof(UnitTable) + (a.view.R_max + 2) * sizeof(int);
+        if (paged && row_tiles == 2) RA_LAUNCH_TIMED((tree_rows_kernel<true, 2>), grid, dim3(256), smem, st, a, n_rowblocks);
+        else if (paged) RA_LAUNCH_TIMED((tree_rows_kernel<true, 1>), grid, dim3(256), smem, st, a, n_rowblocks);
+        else if (row_tiles == 2) RA_LAUNCH_TIMED((tree_rows_kernel<false, 2>), grid, dim3(256), smem, st, a, n_rowblocks);
+        else RA_LAUNCH_TIMED((tree_rows_kernel<false, 1>), grid, dim3(256), smem, st, a, n_rowblocks);
+    } else {
+        const dim3 grid((unsigned)a.S, (unsigned)inner, (unsigned)B);
+        const size_t smem = align_up(SlotTable::bytes(a.view.R_max + 1), 16) + (16 * (D + 4) + D * 20) * sizeof(float);
+        if (D == 128 && paged) RA_LAUNCH_TIMED((tree_f32_kernel<128, true>), grid, dim3(256), smem, st, a, n_rowblocks);
+        else if (D == 128) RA_LAUNCH_TIMED((tree_f32_kernel<128, false>), grid, dim3(256), smem, st, a, n_rowblocks);
+        else if (paged) RA_LAUNCH_TIMED((tree_f32_kernel<64, true>), grid, dim3(256), smem, st, a, n_rowblocks);
+        else RA_LAUNCH_TIMED((tree_f32_kernel<64, false>), grid, dim3(256), smem, st, a, n_rowblocks);
+    }
     if (a.S > 1) launch_combine(a, D, rows, st);
     RA_HIP_CHECK(hipGetLastError());
     return RA_OK;
@@ -251,7 +591,8 @@ extern "C" int ra_round_sparse_attn_tree(ra_ctx* ctx, void* stream, const void* 
     RA_REQUIRE(aligned16(q) && aligned16(layer->k) && aligned16(layer->v) && aligned16(cur_k) && aligned16(cur_v) && aligned16(out),
                RA_ERR_INVALID_ARG, "tree: q, keys, values and out must be 16-byte aligned");
     const TreeOperands tree = {cur_len, tree_mask, tree_len};
-    if (layer->dtype == RA_BF16)
+    const bool bf16 = layer->dtype == RA_BF16;
+    if (bf16 && (layer->d != 128 || n_nodes * G < kTreeRows))  // few rows, or 64 channels: the streaming kernel
         return question_attention(ctx, "tree", stream, q, n_nodes, Hq, layer, sel_idx, n_sel, cur_k, cur_v, cur_cap, scale, out, lse,
                                   nullptr, nullptr, &tree);
     AttnArgs a = {};
@@ -274,7 +615,7 @@ extern "C" int ra_round_sparse_attn_tree(ra_ctx* ctx, void* stream, const void* 
     a.tree_mask = tree_mask;
     a.tree_len = tree_len;
     a.tree_words = (n_nodes + 31) / 32;
-    return tree_attention_f32(ctx, reinterpret_cast<hipStream_t>(stream), a, layer->max_tokens + cur_cap);
+    return tree_attention(ctx, reinterpret_cast<hipStream_t>(stream), a, bf16);
 }
 
 extern "C" int ra_tree_commit(ra_ctx* ctx, void* stream, void* const* cur_k_layers, void* const* cur_v_layers, int n_layers, int B,
