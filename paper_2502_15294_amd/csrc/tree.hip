@@ -56,12 +56,18 @@ __global__ __launch_bounds__(256) void tree_f32_kernel(AttnArgs a, int n_rowbloc
     for (int j = 0; j < D / 16; ++j) acc[j] = floatx4_t{0.f, 0.f, 0.f, 0.f};
     float m = kNegBig, l = 0.f;
 
+    // A thread's share of a unit's keys and values, on their way from memory while the unit before is worked on.
+    struct Unit {
+        float4 k[kQuads], v[kQuads];
+        int tok0, tokens;
+        bool is_cur;
+    };
     int slot = u_lo < u_hi ? find_slot(tab.cum, hdr.n_slots, u_lo) : 0;
-    for (int u = u_lo; u < u_hi; ++u) {
+    auto load = [&](int u) {  // (tokens past the segment's end: its last one again)
+        Unit x;
         while (u >= tab.cum[slot + 1]) ++slot;
         const int len = tab.len[slot], tok0 = (u - tab.cum[slot]) * kUnitTokens, ntok = min(kUnitTokens, len - tok0);
         const bool is_cur = slot >= hdr.n_hist;
-        // ---- the unit's 16 keys and its value tile into LDS (tokens past the segment's end: its last one again) --------
         const float *kp, *vp;
         size_t kstride = D;
         if (is_cur) {
@@ -78,29 +84,39 @@ __global__ __launch_bounds__(256) void tree_f32_kernel(AttnArgs a, int n_rowbloc
             kp = static_cast<const float*>(vw.k) + ((size_t)tab.off_k[slot] * Hkv + (size_t)g * len + tok0) * D;
             vp = static_cast<const float*>(vw.v) + ((size_t)tab.off_v[slot] * Hkv + (size_t)g * ((len + 15) & ~15) + tok0) * D;
         }
-        float4 kx[kQuads], vx[kQuads];
 #pragma unroll
         for (int i = 0; i < kQuads; ++i) {
-            const int x = tid + 256 * i, t = min(x / (D / 4), ntok - 1), c = x % (D / 4) * 4;
-            kx[i] = *reinterpret_cast<const float4*>(kp + (size_t)t * kstride + c);
-            if (is_cur) vx[i] = *reinterpret_cast<const float4*>(vp + (size_t)t * kstride + c);  // four channels of a token
-            else vx[i] = *reinterpret_cast<const float4*>(vp + x * 4);                          // four tokens of a channel
+            const int e = tid + 256 * i, t = min(e / (D / 4), ntok - 1), c = e % (D / 4) * 4;
+            x.k[i] = *reinterpret_cast<const float4*>(kp + (size_t)t * kstride + c);
+            // four channels of a token of the current round, four tokens of a channel of any other
+            x.v[i] = *reinterpret_cast<const float4*>(is_cur ? vp + (size_t)t * kstride + c : vp + e * 4);
         }
+        x.tok0 = tok0;
+        x.tokens = ntok;
+        x.is_cur = is_cur;
+        return x;
+    };
+    Unit x;
+    if (u_lo < u_hi) x = load(u_lo);
+    for (int u = u_lo; u < u_hi; ++u) {
         __syncthreads();  // the unit before is read
 #pragma unroll
         for (int i = 0; i < kQuads; ++i) {
-            const int x = tid + 256 * i, t = x / (D / 4), c = x % (D / 4) * 4;
-            *reinterpret_cast<float4*>(keys + t * kKeyPitch + c) = kx[i];
-            if (is_cur) {
-                values[(c + 0) * kValuePitch + t] = vx[i].x;
-                values[(c + 1) * kValuePitch + t] = vx[i].y;
-                values[(c + 2) * kValuePitch + t] = vx[i].z;
-                values[(c + 3) * kValuePitch + t] = vx[i].w;
+            const int e = tid + 256 * i, t = e / (D / 4), c = e % (D / 4) * 4;
+            *reinterpret_cast<float4*>(keys + t * kKeyPitch + c) = x.k[i];
+            if (x.is_cur) {
+                values[(c + 0) * kValuePitch + t] = x.v[i].x;
+                values[(c + 1) * kValuePitch + t] = x.v[i].y;
+                values[(c + 2) * kValuePitch + t] = x.v[i].z;
+                values[(c + 3) * kValuePitch + t] = x.v[i].w;
             } else {
-                *reinterpret_cast<float4*>(values + x / 4 * kValuePitch + x % 4 * 4) = vx[i];
+                *reinterpret_cast<float4*>(values + e / 4 * kValuePitch + e % 4 * 4) = x.v[i];
             }
         }
         __syncthreads();
+        const int tok0 = x.tok0, ntok = x.tokens;
+        const bool is_cur = x.is_cur;
+        if (u + 1 < u_hi) x = load(u + 1);
         // ---- logits ------------------------------------------------------------------------------------------------
         floatx4_t sc = floatx4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -174,7 +190,7 @@ __global__ __launch_bounds__(256) void tree_f32_kernel(AttnArgs a, int n_rowbloc
 // groups of the values, all with one base address a lane and constant offsets.  So the loop has no segment walk, no block-table
 // look-up and next to no address arithmetic, and one barrier per 64 tokens.  (The question kernel walks the segments in scalar
 // registers, which it has too few of, once per 32 tokens: fourteen vector instructions for every exponential, here nine; 60
-// drafted tokens of 64 heads over 32 paged dialogues of 4 900 tokens: TREE_OLD -> TREE_NEW microseconds.)
+// drafted tokens of 64 heads over 32 paged dialogues of 4 900 tokens: 716 -> 635 microseconds.)
 // Units of the current round, whose values are token-major and whose keys lie Hkv rows apart, take a slower path: their values
 // are gathered by 2-byte loads.
 //
@@ -327,73 +343,88 @@ __global__ __launch_bounds__(256, kTreeWaves) void tree_rows_kernel(AttnArgs a, 
         const int limit = unit < n_units ? tokens & 31 : 0;  // tokens of the lane's unit
         const bool drafts = tokens >= 32 && first + kUnitTokens > committed;
         const bool whole = __all(limit == 16 && !drafts);
+        floatx4_t sc[RT][4];
 #pragma unroll
-        for (int m2 = 0; m2 < 2; ++m2) {  // tokens 8 m2 .. + 7 of every unit
+        for (int h0 = 0; h0 < 4; h0 += 2) {
             uint4 kf[2][4];
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int kk = 0; kk < 4; ++kk) kf[h][kk] = kb[((2 * m2 + h) * 16 + n) * 16 + ((kk * 4 + q4 + n) & 15)];
-            floatx4_t sc[RT][2];
+                for (int kk = 0; kk < 4; ++kk) kf[h][kk] = kb[((h0 + h) * 16 + n) * 16 + ((kk * 4 + q4 + n) & 15)];
 #pragma unroll
             for (int kk = 0; kk < 4; ++kk)  // independent chains interleaved
 #pragma unroll
                 for (int t = 0; t < RT; ++t)
 #pragma unroll
                     for (int h = 0; h < 2; ++h)
-                        sc[t][h] = mfma16(kf[h][kk], q[t][kk], kk ? sc[t][h] : floatx4_t{0.f, 0.f, 0.f, 0.f});
-            if (!whole) {
-#pragma unroll
-                for (int t = 0; t < RT; ++t) {
-                    uint32_t sees = (1u << limit) - 1;
-                    if (drafts)
-                        sees &= tree_sees(a.tree_mask + ((size_t)b * a.q_len + node[t]) * a.tree_words, a.tree_words, first, committed);
-#pragma unroll
-                    for (int h = 0; h < 2; ++h)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            if (!(sees >> (8 * m2 + 4 * h + i) & 1)) sc[t][h][i] = -__builtin_inff();
-                }
-            }
-            bool raise = false;
-            float mx[RT];
+                        sc[t][h0 + h] = mfma16(kf[h][kk], q[t][kk], kk ? sc[t][h0 + h] : floatx4_t{0.f, 0.f, 0.f, 0.f});
+        }
+        if (!whole) {
 #pragma unroll
             for (int t = 0; t < RT; ++t) {
-                mx[t] = max8(sc[t][0], sc[t][1]);
-                raise |= mx[t] > m[t] + slack;
+                uint32_t sees = (1u << limit) - 1;
+                if (drafts)
+                    sees &= tree_sees(a.tree_mask + ((size_t)b * a.q_len + node[t]) * a.tree_words, a.tree_words, first, committed);
+#pragma unroll
+                for (int h = 0; h < 4; ++h)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (!(sees >> (4 * h + i) & 1)) sc[t][h][i] = -__builtin_inff();
             }
-            if (__any(raise)) {
+        }
+        bool raise = false;
+        float mx[RT];
 #pragma unroll
-                for (int t = 0; t < RT; ++t) {
-                    const float m_new = vmax(m[t], xrow_max4(mx[t])), alpha = fast_exp2((m[t] - m_new) * a.c);
-                    l[t] *= alpha;
-#pragma unroll
-                    for (int dt = 0; dt < 8; ++dt) acc[t][dt] *= alpha;
-                    m[t] = m_new;
-                }
-            }
-            uint4 vf[8];  // shared by the row tiles
-#pragma unroll
-            for (int dt = 0; dt < 8; ++dt) vf[dt] = vb[(2 * dt + m2) * 64 + lane];
-            // row tile by row tile: the first one's products can run while the second one's logits become probabilities
+        for (int t = 0; t < RT; ++t) {
+            mx[t] = vmax(max8(sc[t][0], sc[t][1]), max8(sc[t][2], sc[t][3]));
+            raise |= mx[t] > m[t] + slack;
+        }
+        if (__any(raise)) {
 #pragma unroll
             for (int t = 0; t < RT; ++t) {
-                const float mc = m[t] * a.c;
-                float p[8];
+                const float m_new = vmax(m[t], xrow_max4(mx[t])), alpha = fast_exp2((m[t] - m_new) * a.c);
+                l[t] *= alpha;
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
+                for (int dt = 0; dt < 8; ++dt) acc[t][dt] *= alpha;
+                m[t] = m_new;
+            }
+        }
+        // (tokens 8 m2 .. + 7 of every unit, row tile t), one after the other: its products on the matrix cores while the vector ALU
+        // turns the next one's logits into probabilities
+        constexpr int K = 2 * RT;
+        uint4 hi[2], lo[2], vf[8];
+        auto soften = [&](int k) {
+            const int m2 = k / RT, t = k % RT;
+            const float mc = m[t] * a.c;
+            float p[8];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) p[h * 4 + i] = fast_exp2(__builtin_fmaf(sc[t][h][i], a.c, -mc));
-                l[t] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
-                const uint4 hi = make_uint4(pack_nearest(p[0], p[1]), pack_nearest(p[2], p[3]), pack_nearest(p[4], p[5]), pack_nearest(p[6], p[7]));
-                const uint4 lo = make_uint4(
-                    pack_nearest(p[0] - low_bf16(hi.x), p[1] - high_bf16(hi.x)), pack_nearest(p[2] - low_bf16(hi.y), p[3] - high_bf16(hi.y)),
-                    pack_nearest(p[4] - low_bf16(hi.z), p[5] - high_bf16(hi.z)), pack_nearest(p[6] - low_bf16(hi.w), p[7] - high_bf16(hi.w)));
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int dt = 0; dt < 8; ++dt) {
-                    acc[t][dt] = mfma16(vf[dt], hi, acc[t][dt]);
-                    acc[t][dt] = mfma16(vf[dt], lo, acc[t][dt]);
-                }
+                for (int i = 0; i < 4; ++i) p[h * 4 + i] = fast_exp2(__builtin_fmaf(sc[t][2 * m2 + h][i], a.c, -mc));
+            l[t] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+            const uint4 x = make_uint4(pack_nearest(p[0], p[1]), pack_nearest(p[2], p[3]), pack_nearest(p[4], p[5]), pack_nearest(p[6], p[7]));
+            hi[k & 1] = x;
+            lo[k & 1] = make_uint4(
+                pack_nearest(p[0] - low_bf16(x.x), p[1] - high_bf16(x.x)), pack_nearest(p[2] - low_bf16(x.y), p[3] - high_bf16(x.y)),
+                pack_nearest(p[4] - low_bf16(x.z), p[5] - high_bf16(x.z)), pack_nearest(p[6] - low_bf16(x.w), p[7] - high_bf16(x.w)));
+        };
+        soften(0);
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int m2 = k / RT, t = k % RT;
+            if (t == 0) {
+#pragma unroll
+                for (int dt = 0; dt < 8; ++dt) vf[dt] = vb[(2 * dt + m2) * 64 + lane];
+            }
+            if (k + 1 < K) soften(k + 1);
+#pragma unroll
+            for (int dt = 0; dt < 8; ++dt) acc[t][dt] = mfma16(vf[dt], hi[k & 1], acc[t][dt]);
+#pragma unroll
+            for (int dt = 0; dt < 8; ++dt) acc[t][dt] = mfma16(vf[dt], lo[k & 1], acc[t][dt]);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // a product
+                __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);  // four vector instructions
             }
         }
     };
@@ -481,7 +512,14 @@ static int tree_pieces(long long items, long long at_once, int64_t max_units, in
     return (int)std::min<int64_t>(4, most);
 }
 
-constexpr int kTreeRows = 17;  // query rows per KV head from which the waves share keys and values through LDS
+// Which kernel a bf16 tree with 128 channels gets (microseconds of whole calls, left the question kernels):
+//   up to 16 query rows per KV head: the streaming kernel, which reads the keys once for 16 rows;
+//   17 to 32: that kernel would read them twice (32 paged dialogues of 4 900 tokens, 24 rows: 197 and 150 here; 8 dialogues of
+//     3 300, 20 rows: 50.3 and 41.6, 32 rows: 51.3 and 43.6);
+//   more: the question kernel where it plans itself, with ranges that are equal over the whole batch (8 dialogues, 100 rows: 53.3
+//     and 58.9; 32: 135 and 149; 12 paged ones, 480 rows: 269 and 276), this file's where it does not (32 paged dialogues of 50
+//     rounds, 64 rows: 196 and 160, 128: 243 and 199, 480: 716 and 635; contiguous 616 and 606).
+static bool tree_by_units(int B, int R_max, int rows) { return rows > 16 && (rows <= 32 || !attn_mfma_plans_inline(B, R_max)); }
 
 static int tree_attention(ra_ctx* ctx, hipStream_t st, AttnArgs& a, bool bf16) {
     const int B = a.view.B, Hkv = a.view.Hkv, D = a.view.d, rows_total = a.q_len * a.G;
@@ -493,9 +531,8 @@ static int tree_attention(ra_ctx* ctx, hipStream_t st, AttnArgs& a, bool bf16) {
     const int64_t max_tokens = a.max_tokens + a.cur_cap;
     RA_REQUIRE(max_tokens < (int64_t)1 << 30, RA_ERR_UNSUPPORTED, "tree: max_tokens too large");
     const size_t rows = (size_t)B * rows_total * Hkv;
-    a.min_units = 8;  // 128 tokens
-    a.S = bf16 ? tree_pieces(inner * B, (long long)kTreeWaves * ctx->num_cu, max_tokens / kUnitTokens, a.min_units)
-               : decode_splits(ctx->num_cu, B, (int)inner, max_tokens);
+    a.min_units = bf16 ? 8 : 2;  // (fp32 calls are small: one dialogue of 500 tokens)
+    a.S = tree_pieces(inner * B, (long long)kTreeWaves * ctx->num_cu, max_tokens / kUnitTokens, a.min_units);
     AttnWorkspace w = attn_workspace(rows, a.S, D, B, a.view.R_max);
     while (a.S > 1 && w.total > ctx->ws.bytes) w = attn_workspace(rows, --a.S, D, B, a.view.R_max);
     RA_REQUIRE(ctx->ws.base != nullptr && ctx->ws.bytes >= w.total, RA_ERR_WORKSPACE,
@@ -592,7 +629,7 @@ extern "C" int ra_round_sparse_attn_tree(ra_ctx* ctx, void* stream, const void* 
                RA_ERR_INVALID_ARG, "tree: q, keys, values and out must be 16-byte aligned");
     const TreeOperands tree = {cur_len, tree_mask, tree_len};
     const bool bf16 = layer->dtype == RA_BF16;
-    if (bf16 && (layer->d != 128 || n_nodes * G < kTreeRows))  // few rows, or 64 channels: the streaming kernel
+    if (bf16 && (layer->d != 128 || !tree_by_units(layer->B, layer->R_max, n_nodes * G)))  // (64 channels: the streaming kernel)
         return question_attention(ctx, "tree", stream, q, n_nodes, Hq, layer, sel_idx, n_sel, cur_k, cur_v, cur_cap, scale, out, lse,
                                   nullptr, nullptr, &tree);
     AttnArgs a = {};
