@@ -58,11 +58,18 @@ __global__ __launch_bounds__(256) void tree_f32_kernel(AttnArgs a, int n_rowbloc
 
     // A thread's share of a unit's keys and values, on their way from memory while the unit before is worked on.
     struct Unit {
-        float4 k[kQuads], v[kQuads];
+        floatx4_t k[kQuads], v[kQuads];
         int tok0, tokens;
         bool is_cur;
     };
-    int slot = u_lo < u_hi ? find_slot(tab.cum, hdr.n_slots, u_lo) : 0;
+    if (u_lo >= u_hi) {  // an empty key set (one piece)
+        if (!row_ok) return;
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) *reinterpret_cast<floatx4_t*>(a.out + rowid * D + 16 * j + 4 * q4) = acc[j];
+        if (a.lse && q4 == 0) a.lse[rowid] = -__builtin_inff();
+        return;
+    }
+    int slot = find_slot(tab.cum, hdr.n_slots, u_lo);
     auto load = [&](int u) {  // (tokens past the segment's end: its last one again)
         Unit x;
         while (u >= tab.cum[slot + 1]) ++slot;
@@ -87,36 +94,35 @@ __global__ __launch_bounds__(256) void tree_f32_kernel(AttnArgs a, int n_rowbloc
 #pragma unroll
         for (int i = 0; i < kQuads; ++i) {
             const int e = tid + 256 * i, t = min(e / (D / 4), ntok - 1), c = e % (D / 4) * 4;
-            x.k[i] = *reinterpret_cast<const float4*>(kp + (size_t)t * kstride + c);
+            x.k[i] = *reinterpret_cast<const floatx4_t*>(kp + (size_t)t * kstride + c);
             // four channels of a token of the current round, four tokens of a channel of any other
-            x.v[i] = *reinterpret_cast<const float4*>(is_cur ? vp + (size_t)t * kstride + c : vp + e * 4);
+            x.v[i] = *reinterpret_cast<const floatx4_t*>(is_cur ? vp + (size_t)t * kstride + c : vp + e * 4);
         }
         x.tok0 = tok0;
         x.tokens = ntok;
         x.is_cur = is_cur;
         return x;
     };
-    Unit x;
-    if (u_lo < u_hi) x = load(u_lo);
+    Unit x = load(u_lo);
     for (int u = u_lo; u < u_hi; ++u) {
         __syncthreads();  // the unit before is read
 #pragma unroll
         for (int i = 0; i < kQuads; ++i) {
             const int e = tid + 256 * i, t = e / (D / 4), c = e % (D / 4) * 4;
-            *reinterpret_cast<float4*>(keys + t * kKeyPitch + c) = x.k[i];
+            *reinterpret_cast<floatx4_t*>(keys + t * kKeyPitch + c) = x.k[i];
             if (x.is_cur) {
-                values[(c + 0) * kValuePitch + t] = x.v[i].x;
-                values[(c + 1) * kValuePitch + t] = x.v[i].y;
-                values[(c + 2) * kValuePitch + t] = x.v[i].z;
-                values[(c + 3) * kValuePitch + t] = x.v[i].w;
+                values[(c + 0) * kValuePitch + t] = x.v[i][0];
+                values[(c + 1) * kValuePitch + t] = x.v[i][1];
+                values[(c + 2) * kValuePitch + t] = x.v[i][2];
+                values[(c + 3) * kValuePitch + t] = x.v[i][3];
             } else {
-                *reinterpret_cast<float4*>(values + e / 4 * kValuePitch + e % 4 * 4) = x.v[i];
+                *reinterpret_cast<floatx4_t*>(values + e / 4 * kValuePitch + e % 4 * 4) = x.v[i];
             }
         }
         __syncthreads();
         const int tok0 = x.tok0, ntok = x.tokens;
         const bool is_cur = x.is_cur;
-        if (u + 1 < u_hi) x = load(u + 1);
+        x = load(min(u + 1, u_hi - 1));  // (in any case: a load behind a condition would be waited for where the paths meet)
         // ---- logits ------------------------------------------------------------------------------------------------
         floatx4_t sc = floatx4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -568,7 +574,7 @@ static int tree_attention(ra_ctx* ctx, hipStream_t st, AttnArgs& a, bool bf16) {
 // ---- the accepted path ---------------------------------------------------------------------------------------------------
 constexpr int kCommitLayers = 32;  // layers of one launch (their pointers are kernel arguments)
 struct CommitLayers {
-    uint4* p[2 * kCommitLayers];
+    u32x4_t* p[2 * kCommitLayers];
 };
 constexpr int kCommitFlight = 8;  // rows that a thread has in flight
 
@@ -590,12 +596,12 @@ __global__ __launch_bounds__(256) void tree_commit_kernel(CommitLayers layers, i
     }
     if (new_len && blockIdx.y == 0 && blockIdx.z == 0 && threadIdx.x == 0) new_len[b] = committed + n;
     if (column >= row16) return;
-    uint4* rows = layers.p[blockIdx.y] + ((size_t)b * cur_cap + committed) * row16 + column;
+    u32x4_t* rows = layers.p[blockIdx.y] + ((size_t)b * cur_cap + committed) * row16 + column;
     for (int j0 = 0; j0 < n; j0 += kCommitFlight) {
-        uint4 v[kCommitFlight];
+        u32x4_t v[kCommitFlight];
 #pragma unroll
         for (int i = 0; i < kCommitFlight; ++i)
-            if (j0 + i < n) v[i] = rows[(size_t)path[j0 + i] * row16];
+            v[i] = rows[(size_t)path[min(j0 + i, n - 1)] * row16];  // (behind the last one: that one again, not written)
 #pragma unroll
         for (int i = 0; i < kCommitFlight; ++i)
             if (j0 + i < n) rows[(size_t)(j0 + i) * row16] = v[i];
@@ -676,8 +682,8 @@ extern "C" int ra_tree_commit(ra_ctx* ctx, void* stream, void* const* cur_k_laye
         CommitLayers layers = {};
         const int n = n_layers - l0 < kCommitLayers ? n_layers - l0 : kCommitLayers;
         for (int l = 0; l < n; ++l) {
-            layers.p[2 * l] = static_cast<uint4*>(cur_k_layers[l0 + l]);
-            layers.p[2 * l + 1] = static_cast<uint4*>(cur_v_layers[l0 + l]);
+            layers.p[2 * l] = static_cast<u32x4_t*>(cur_k_layers[l0 + l]);
+            layers.p[2 * l + 1] = static_cast<u32x4_t*>(cur_v_layers[l0 + l]);
         }
         hipLaunchKernelGGL(tree_commit_kernel, dim3((unsigned)B, (unsigned)(2 * n), (unsigned)columns), dim3(256), 0,
                            reinterpret_cast<hipStream_t>(stream), layers, cur_cap, (int)(row_bytes / 16), cur_len, path, n_path,
