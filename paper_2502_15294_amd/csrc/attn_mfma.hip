@@ -150,7 +150,7 @@ __global__ __launch_bounds__(256) void merge_records_kernel(AttnArgs a, int n_ro
 // TREE: the query tokens are drafted ones, of which every one sees the committed tokens of the current round and its ancestors.
 template <int D, bool PAGED, bool TILE_LSE, bool INLINE_PLAN, bool MAYBE_LONG, bool TREE>
 __global__ __launch_bounds__(256, 2) void attn_mfma_kernel(AttnArgs a, int n_rowblocks) {
-    constexpr int KK = D / 32, DT = D / 16, kParts = D == 64 ? 3 : 2;  // contraction steps of Q.K^T, 16-channel tiles of the output,
+    constexpr int KK = D / 32, DT = D / 16, kParts = D == 64 || TREE ? 3 : 2;  // contraction steps of Q.K^T, 16-channel tiles of the output,
                                                                         // bf16 numbers a probability is carried as
     extern __shared__ __align__(16) char smem[];
     // Tiles of every sequence and their prefix; planned inline every wave keeps the prefix (and the cut below) for itself, so that
@@ -658,12 +658,9 @@ __global__ __launch_bounds__(256, 2) void attn_mfma_kernel(AttnArgs a, int n_row
                 // (the compiler's iterative-ilp schedule, which the tests compare with, crashes on 64 channels without the fence)
                 if (D == 64) __builtin_amdgcn_sched_barrier(0);
                 uint4 ph[kParts];
-                if constexpr (TREE && D == 128) {  // both parts to the nearest: a weight is off by 2^-18 of itself at most, of either sign
-                    ph[0] = make_uint4(pack_nearest(p[0], p[1]), pack_nearest(p[2], p[3]), pack_nearest(p[4], p[5]), pack_nearest(p[6], p[7]));
-                    ph[1] = make_uint4(pack_nearest(p[0] - low_bf16(ph[0].x), p[1] - high_bf16(ph[0].x)),
-                                       pack_nearest(p[2] - low_bf16(ph[0].y), p[3] - high_bf16(ph[0].y)),
-                                       pack_nearest(p[4] - low_bf16(ph[0].z), p[5] - high_bf16(ph[0].z)),
-                                       pack_nearest(p[6] - low_bf16(ph[0].w), p[7] - high_bf16(ph[0].w)));
+                if constexpr (TREE && D == 128) {
+#pragma unroll
+                    for (int i = 0; i < kParts; ++i) ph[i] = take_part(p, i + 1 == kParts);
                 }
 #pragma unroll
                 for (int i = 0; i < kParts && !(TREE && D == 128); ++i) {

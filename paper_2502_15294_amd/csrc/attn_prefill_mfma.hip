@@ -432,7 +432,7 @@ __global__ __launch_bounds__(256, kWorkgroupsPerCuP) void attn_prefill_mfma_kern
             uint4 vf[8];  // V^T operand fragments of the tile, shared by both row tiles
 #pragma unroll
             for (int dt = 0; dt < 8; ++dt) vf[dt] = vb[dt * 64 + lane];
-            auto probabilities = [&](int nt, uint4& phi, uint4& plo) {  // P (hi + lo, or fp16) of row tile nt, and its row sums
+            auto probabilities = [&](int nt, uint4& phi, uint4& plo, uint4& prest) {  // P (hi + lo, or fp16) of row tile nt, and its row sums
                 const float mc = m[nt] * a.c - (P_HALF ? (float)kHalfScaleLog2 : 0.f);
                 float p[8];
 #pragma unroll
@@ -454,12 +454,10 @@ __global__ __launch_bounds__(256, kWorkgroupsPerCuP) void attn_prefill_mfma_kern
                 } else {
                     const float ps = ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
                     l[nt] += ps;
-                    if constexpr (TREE) {  // both parts to the nearest: a weight is off by 2^-18 of itself at most, of either sign
-                        phi = make_uint4(pack_nearest(p[0], p[1]), pack_nearest(p[2], p[3]), pack_nearest(p[4], p[5]), pack_nearest(p[6], p[7]));
-                        plo = make_uint4(pack_nearest(p[0] - low_bf16(phi.x), p[1] - high_bf16(phi.x)),
-                                         pack_nearest(p[2] - low_bf16(phi.y), p[3] - high_bf16(phi.y)),
-                                         pack_nearest(p[4] - low_bf16(phi.z), p[5] - high_bf16(phi.z)),
-                                         pack_nearest(p[6] - low_bf16(phi.w), p[7] - high_bf16(phi.w)));
+                    if constexpr (TREE) {  // three parts: as exact as the plain form in 32 bits
+                        phi = take_part(p, false);
+                        plo = take_part(p, false);
+                        prest = take_part(p, true);
                         return;
                     }
                     phi.x = pack_hi16(p[0], p[1]);
@@ -472,7 +470,7 @@ __global__ __launch_bounds__(256, kWorkgroupsPerCuP) void attn_prefill_mfma_kern
                     plo.w = pack_hi16(p[6] - trunc_bf16(p[6]), p[7] - trunc_bf16(p[7]));
                 }
             };
-            auto accumulate = [&](int nt, const uint4& phi, const uint4& plo) {
+            auto accumulate = [&](int nt, const uint4& phi, const uint4& plo, const uint4& prest) {
 #pragma unroll
                 for (int dt = 0; dt < 8; ++dt) {
                     if constexpr (P_HALF) {
@@ -480,6 +478,7 @@ __global__ __launch_bounds__(256, kWorkgroupsPerCuP) void attn_prefill_mfma_kern
                     } else {
                         acc[nt][dt] = mfma16(vf[dt], phi, acc[nt][dt]);
                         acc[nt][dt] = mfma16(vf[dt], plo, acc[nt][dt]);
+                        if constexpr (TREE) acc[nt][dt] = mfma16(vf[dt], prest, acc[nt][dt]);
                     }
                 }
             };
@@ -487,9 +486,9 @@ __global__ __launch_bounds__(256, kWorkgroupsPerCuP) void attn_prefill_mfma_kern
             // turns the second tile's logits into probabilities.
 #pragma unroll
             for (int nt = 0; nt < N; ++nt) {
-                uint4 phi, plo;
-                probabilities(nt, phi, plo);
-                accumulate(nt, phi, plo);
+                uint4 phi, plo, prest;
+                probabilities(nt, phi, plo, prest);
+                accumulate(nt, phi, plo, prest);
             }
         };
 

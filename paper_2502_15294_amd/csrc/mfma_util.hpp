@@ -41,5 +41,15 @@ __device__ __forceinline__ uint32_t pack_nearest(float a, float b) {
 }
 __device__ __forceinline__ float low_bf16(uint32_t pair) { return as_f32(pair << 16); }
 __device__ __forceinline__ float high_bf16(uint32_t pair) { return as_f32(pair & 0xffff0000u); }
+// Eight floats as sums of three bf16 numbers each, part by part, every part to the nearest: all of a float's 24 bits.  p holds what
+// is left.
+__device__ __forceinline__ uint4 take_part(float (&p)[8], bool last) {
+    const uint4 x = make_uint4(pack_nearest(p[0], p[1]), pack_nearest(p[2], p[3]), pack_nearest(p[4], p[5]), pack_nearest(p[6], p[7]));
+    if (!last) {
+        p[0] -= low_bf16(x.x), p[1] -= high_bf16(x.x), p[2] -= low_bf16(x.y), p[3] -= high_bf16(x.y);
+        p[4] -= low_bf16(x.z), p[5] -= high_bf16(x.z), p[6] -= low_bf16(x.w), p[7] -= high_bf16(x.w);
+    }
+    return x;
+}
 
 }  // namespace ra

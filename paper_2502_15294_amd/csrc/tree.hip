@@ -200,7 +200,8 @@ __global__ __launch_bounds__(256) void tree_f32_kernel(AttnArgs a, int n_rowbloc
 // Units of the current round, whose values are token-major and whose keys lie Hkv rows apart, take a slower path: their values
 // are gathered by 2-byte loads.
 //
-// P goes to the matrix cores as the sum of two bf16 numbers, both rounded to the nearest: a weight is off by 2^-18 of itself at most.
+// P goes to the matrix cores as the sum of three bf16 numbers, which hold all of its 24 bits.  (With two, both rounded to the
+// nearest, outputs were off by 2.5e-6 of themselves, twice what fp32 arithmetic is.)
 constexpr int kUnitsAhead = 256;                    // units that are looked up at a time
 constexpr int kStepUnits = 4, kStepBytes = 32768;   // 16 KB of keys, 16 KB of values
 constexpr int kTreeWaves = 2;                       // workgroups of a compute unit, waves of a SIMD
@@ -398,7 +399,7 @@ __global__ __launch_bounds__(256, kTreeWaves) void tree_rows_kernel(AttnArgs a, 
         // (tokens 8 m2 .. + 7 of every unit, row tile t), one after the other: its products on the matrix cores while the vector ALU
         // turns the next one's logits into probabilities
         constexpr int K = 2 * RT;
-        uint4 hi[2], lo[2], vf[8];
+        uint4 part[2][3], vf[8];
         auto soften = [&](int k) {
             const int m2 = k / RT, t = k % RT;
             const float mc = m[t] * a.c;
@@ -408,11 +409,8 @@ __global__ __launch_bounds__(256, kTreeWaves) void tree_rows_kernel(AttnArgs a, 
 #pragma unroll
                 for (int i = 0; i < 4; ++i) p[h * 4 + i] = fast_exp2(__builtin_fmaf(sc[t][2 * m2 + h][i], a.c, -mc));
             l[t] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
-            const uint4 x = make_uint4(pack_nearest(p[0], p[1]), pack_nearest(p[2], p[3]), pack_nearest(p[4], p[5]), pack_nearest(p[6], p[7]));
-            hi[k & 1] = x;
-            lo[k & 1] = make_uint4(
-                pack_nearest(p[0] - low_bf16(x.x), p[1] - high_bf16(x.x)), pack_nearest(p[2] - low_bf16(x.y), p[3] - high_bf16(x.y)),
-                pack_nearest(p[4] - low_bf16(x.z), p[5] - high_bf16(x.z)), pack_nearest(p[6] - low_bf16(x.w), p[7] - high_bf16(x.w)));
+#pragma unroll
+            for (int i = 0; i < 3; ++i) part[k & 1][i] = take_part(p, i == 2);
         };
         soften(0);
 #pragma unroll
@@ -424,11 +422,11 @@ __global__ __launch_bounds__(256, kTreeWaves) void tree_rows_kernel(AttnArgs a, 
             }
             if (k + 1 < K) soften(k + 1);
 #pragma unroll
-            for (int dt = 0; dt < 8; ++dt) acc[t][dt] = mfma16(vf[dt], hi[k & 1], acc[t][dt]);
+            for (int i = 0; i < 3; ++i)
 #pragma unroll
-            for (int dt = 0; dt < 8; ++dt) acc[t][dt] = mfma16(vf[dt], lo[k & 1], acc[t][dt]);
+                for (int dt = 0; dt < 8; ++dt) acc[t][dt] = mfma16(vf[dt], part[k & 1][i], acc[t][dt]);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
+            for (int i = 0; i < 24; ++i) {
                 __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // a product
                 __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);  // four vector instructions
             }
