@@ -136,7 +136,7 @@ int ra_set_workspace(ra_ctx* ctx, void* device_ptr, size_t bytes);
 /*
  * Measurement aid (Sec. 4.3 and App. C break the latency down into the selection and attention steps; this is
  * how a benchmark gets the duration of the kernel that dominates a call, without the small kernels around it).
- * While enabled, ra_round_scores, ra_round_sparse_attn_decode and ra_round_sparse_attn_prefill attach two HIP
+ * While enabled, ra_round_scores, ra_round_sparse_attn_decode, _prefill and _tree, and ra_token_weights attach two HIP
  * events to the launch of their streaming kernel (the pass over the keys, or over the selected keys and
  * values), which then carry that kernel's own start and end time stamps.  ra_profile_last_ms waits for the end
  * event of the most recent such call and returns the milliseconds between the two; RA_ERR_STATE if no call was
@@ -414,7 +414,8 @@ typedef struct ra_keep_params {
  *   kept_off   device int64 [B][R_max] or NULL: a place for every round, packed in whole 16-token blocks behind b * stride,
  *              in tokens (seg_off and seg_off_v of a contiguous cache) or slots (seg_off of a paged one)
  *   kept_weights   device float [B][n_pos] or NULL: the kept tokens' weights at their new positions, 0 behind the last;
- *              another buffer than `weights`
+ *              another buffer than `weights`.  (With it, sequences of many positions are several workgroups': their counts
+ *              lie there until the weights do)
  * n_pos <= 2^24.  No workspace is used.
  */
 int ra_select_tokens(ra_ctx* ctx, void* stream, const float* weights, int n_pos, const int32_t* seg_len,

@@ -160,6 +160,24 @@ def test_selection_sizes(n, R, budget):
     check_selection(w, lens, np.full(3, R), budget, first=min(16, budget // 4), last=budget // 8)
 
 
+@pytest.mark.parametrize("kind", list(WEIGHTS) + ["mostly_zero"])
+@pytest.mark.parametrize("budget,first,last", [(1, 0, 0), (20000, 100, 300), (400, 100, 300), (69999, 0, 0), (90000, 5, 5)])
+def test_selection_by_several_workgroups(kind, budget, first, last):
+    """From 65536 positions on a sequence is several workgroups': every kind of weights, short and empty sequences among them."""
+    rng = np.random.default_rng(budget)
+    n_pos = 80000
+    lens = np.zeros((4, 150), dtype=np.int32)
+    lens[0] = rng.multinomial(70001, np.ones(150) / 150)
+    lens[1, :3] = [16384, 1, 16383]  # ends where a workgroup's part does
+    lens[2, 140:] = 9999  # more than there are positions
+    n_rounds = np.array([150, 3, 150, 0])
+    if kind == "mostly_zero":
+        w = np.where(rng.random((4, n_pos)) < 0.97, 0.0, rng.random((4, n_pos))).astype(np.float32)
+    else:
+        w = WEIGHTS[kind](rng, (4, n_pos)).astype(np.float32)
+    check_selection(w, lens, n_rounds, budget, first, last, block_size=16 if first else 0, stride=200000)
+
+
 def test_positions_behind_the_weights_are_not_there():
     w = np.linspace(0, 1, 50, dtype=np.float32)[None].repeat(2, 0)
     check_selection(w, np.array([[30, 40, 5], [10, 10, 10]], dtype=np.int32), np.array([3, 3]), 20, 3, 5)

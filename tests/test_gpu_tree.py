@@ -99,7 +99,7 @@ def test_sizes(dtype, Hkv, G, d, n, cap):
 
 
 @pytest.mark.parametrize("lens", ["many_sequences", "many_rounds", "one_round"])
-@pytest.mark.parametrize("dtype,G,d,n", [("bf16", 4, 128, 5), ("bf16", 4, 128, 40), ("bf16", 2, 64, 20), ("f32", 2, 64, 9)])
+@pytest.mark.parametrize("dtype,G,d,n", [("bf16", 4, 128, 3), ("bf16", 4, 128, 5), ("bf16", 4, 128, 40), ("bf16", 2, 64, 20), ("f32", 2, 64, 9)])
 def test_batches(lens, dtype, G, d, n):
     run_tree(LENS[lens], 2, G, d, dtype, n, n + 30, paged=G == 4, seed=3, select=lens != "one_round")
 
@@ -161,6 +161,12 @@ def test_lengths_out_of_range_are_clamped():
         ref, _ = ra.ra_round_sparse_attn_tree(ctx, q, cache.view, mask, ck, cv, ints(0, 8, cap), tree_len=ints(n, cap - 8, 0))
         assert torch.equal(out, ref) and out[2].abs().max().item() == 0
         ra.ra_destroy(ctx)
+
+
+def test_tokens_far_into_a_long_round():
+    """One round of 70 000 tokens, more units than a workgroup looks up at a time."""
+    run_tree([[70000], [9]], 1, 4, 128, "bf16", 5, 20, paged=True, seed=8, select=False)
+    run_tree([[40000, 3] + [1] * 700] * 2, 1, 8, 128, "bf16", 9, 20, paged=False, seed=9, select=False)
 
 
 # ---- the accepted path -------------------------------------------------------------------------------------------------
