@@ -502,18 +502,19 @@ __global__ __launch_bounds__(256, kTreeWaves) void tree_rows_kernel(AttnArgs a, 
     }
 }
 
-// Pieces that every sequence is cut into at most, for `items` workgroups a piece of which `at_once` run at the same time: as many
-// as those, or, if there are more items than that, the fewest pieces with which the last turn is nearly full.
+// Pieces that every sequence is cut into at most, for `items` workgroups a piece of which `at_once` run at the same time: the
+// number with which the turns of workgroups take the least time, a two-hundredth of a whole sequence reckoned for every piece's
+// start and merge.
 static int tree_pieces(long long items, long long at_once, int64_t max_units, int min_units) {
     int64_t most = max_units / min_units;
-    if (most < 1) most = 1;
-    if (most > 64) most = 64;
-    if (items < at_once) return (int)std::min<int64_t>(at_once / items, most);
-    for (int S = 1; S <= 4 && S <= most; ++S) {
-        const long long turns = (items * S + at_once - 1) / at_once;
-        if (turns * at_once * 8 <= items * S * 9) return S;
+    most = most < 1 ? 1 : most > 64 ? 64 : most;
+    int best = 1;
+    double least = 1e30;
+    for (int S = 1; S <= most; ++S) {
+        const double cost = (double)((items * S + at_once - 1) / at_once) / S + 0.005 * S;
+        if (cost < least) least = cost, best = S;
     }
-    return (int)std::min<int64_t>(4, most);
+    return best;
 }
 
 // Which kernel a bf16 tree with 128 channels gets (microseconds of whole calls, left the question kernels):
