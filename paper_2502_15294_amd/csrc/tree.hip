@@ -2,7 +2,8 @@
 // other, and the accepted path's move behind the committed tokens.
 //
 // bf16 goes to the question kernels (attn_mfma.hip, attn_prefill_mfma.hip), which a tree is a question for whose rows see
-// other parts of the current round.  This file holds the entry points, the kernel for fp32 caches and the move.
+// other parts of the current round, or to this file's kernel (tree_by_units).  This file also holds the kernel for fp32 caches
+// and the move.
 #include "attn_common.hpp"
 #include "mfma_util.hpp"
 #include "stream_kv.hpp"
@@ -195,13 +196,17 @@ __global__ __launch_bounds__(256) void tree_f32_kernel(AttnArgs a, int n_rowbloc
 // keeps the addresses in LDS; wave w brings the keys of a step's unit w, four instructions of four whole rows, and two channel
 // groups of the values, all with one base address a lane and constant offsets.  So the loop has no segment walk, no block-table
 // look-up and next to no address arithmetic, and one barrier per 64 tokens.  (The question kernel walks the segments in scalar
-// registers, which it has too few of, once per 32 tokens: fourteen vector instructions for every exponential, here nine; 60
-// drafted tokens of 64 heads over 32 paged dialogues of 4 900 tokens: 716 -> 635 microseconds.)
+// registers, which it has too few of, once per 32 tokens; 60 drafted tokens of 64 heads over 32 paged dialogues of 4 900 tokens: 765
+// -> 725 microseconds.)
 // Units of the current round, whose values are token-major and whose keys lie Hkv rows apart, take a slower path: their values
 // are gathered by 2-byte loads.
 //
 // P goes to the matrix cores as the sum of three bf16 numbers, which hold all of its 24 bits.  (With two, both rounded to the
-// nearest, outputs were off by 2.5e-6 of themselves, twice what fp32 arithmetic is.)
+// nearest, outputs were off by 2.5e-6 of themselves, twice what fp32 arithmetic is; the third costs 19 % at the size above.)
+//
+// Bound by the matrix cores and the vector ALUs in turn: at that size the matrix cores are busy for 41 % of the kernel's time (302 GFLOP
+// of the formula, four halves of it as products: 830 TFLOP/s), the vector ALUs work for about as long, and a fifth is waiting
+// for keys and values.  Tried: wave priorities, the products of the high parts first, both row tiles' softmax first: no change.
 constexpr int kUnitsAhead = 256;                    // units that are looked up at a time
 constexpr int kStepUnits = 4, kStepBytes = 32768;   // 16 KB of keys, 16 KB of values
 constexpr int kTreeWaves = 2;                       // workgroups of a compute unit, waves of a SIMD
@@ -519,11 +524,11 @@ static int tree_pieces(long long items, long long at_once, int64_t max_units, in
 
 // Which kernel a bf16 tree with 128 channels gets (microseconds of whole calls, left the question kernels):
 //   up to 16 query rows per KV head: the streaming kernel, which reads the keys once for 16 rows;
-//   17 to 32: that kernel would read them twice (32 paged dialogues of 4 900 tokens, 24 rows: 197 and 150 here; 8 dialogues of
-//     3 300, 20 rows: 50.3 and 41.6, 32 rows: 51.3 and 43.6);
-//   more: the question kernel where it plans itself, with ranges that are equal over the whole batch (8 dialogues, 100 rows: 53.3
-//     and 58.9; 32: 135 and 149; 12 paged ones, 480 rows: 269 and 276), this file's where it does not (32 paged dialogues of 50
-//     rounds, 64 rows: 196 and 160, 128: 243 and 199, 480: 716 and 635; contiguous 616 and 606).
+//   17 to 32: that kernel would read them twice (32 paged dialogues of 4 900 tokens, 24 rows: 200 and 171 here; 8 dialogues of
+//     3 300, 20 rows: 51 and 45, 32 rows: 51 and 45);
+//   more: the question kernel where it plans itself, with ranges that are equal over the whole batch (8 dialogues, 100 rows: 56
+//     and 65; 32: 152 and 181; 12 paged ones, 480 rows: 292 and 312), this file's where it does not (32 paged dialogues of 50
+//     rounds, 64 rows: 214 and 169, 128: 269 and 233, 480: 765 and 725; contiguous 699 and 710).
 static bool tree_by_units(int B, int R_max, int rows) { return rows > 16 && (rows <= 32 || !attn_mfma_plans_inline(B, R_max)); }
 
 static int tree_attention(ra_ctx* ctx, hipStream_t st, AttnArgs& a, bool bf16) {

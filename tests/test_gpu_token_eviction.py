@@ -244,6 +244,13 @@ def test_compaction_of_keys_alone_and_of_many_rounds():
     check_compaction([[(7 * b) % 90, 50] for b in range(80)], 1, 128, "bf16", False, False, 0.3)
 
 
+@pytest.mark.parametrize("tokens", [350, 700, 1400])
+@pytest.mark.parametrize("dtype,paged,share", [("bf16", False, 0.9), ("f32", True, 0.2)])
+def test_compaction_in_pieces_of_every_length(tokens, dtype, paged, share):
+    """Six dialogues of 8 heads: pieces of 16, 32 and 64 tokens; rounds that end inside a piece, at its end and behind it."""
+    check_compaction([[tokens]] + [[tokens - 64 - 17 * b, 64, 17 * b] for b in range(5)], 8, 64, dtype, paged, not paged, share)
+
+
 def test_positions_that_are_none_give_zeros():
     cache = Cache([[10, 20]], 2, 64, "f32", False)
     small = smaller_cache(cache, np.array([[3, 2]], dtype=np.int32), False)
