@@ -129,9 +129,8 @@ struct DigitCounts {
     int here;        // ... of so many candidates
     int wave_sum[kSelWaves];
 };
-__device__ __forceinline__ void clear_counts(DigitCounts& d) {  // ends with a barrier
+__device__ __forceinline__ void clear_counts(DigitCounts& d) {  // no barrier
     for (int i = threadIdx.x; i < kBins; i += kSelThreads) *reinterpret_cast<int4*>(&d.hist[4 * i]) = make_int4(0, 0, 0, 0);
-    __syncthreads();
 }
 __device__ __forceinline__ int count_of(const DigitCounts& d, int bin) {
     const int4 four = *reinterpret_cast<const int4*>(&d.hist[bin * 4]);
@@ -192,7 +191,7 @@ __device__ __forceinline__ void count_digit(DigitCounts& d, const TokenRange& ra
 }
 
 // Writes the kept positions of the wave's chunks: kept for certain before them `sure`, with the threshold's key `ties`.
-// below(round, kept positions below its start) for the rounds that start in the chunks; keep(place, position, weight).
+// below(round, kept positions below its start), by any lane, for the rounds that start in the chunks; keep(place, position, weight).
 // 0: dropped, 1: kept, 2: kept if it is among the first `equal` of its kind
 __device__ __forceinline__ int fate(const TokenRange& range, const Threshold& t, int p0, int p, float x) {
     const uint32_t key = weight_key(x);
@@ -235,13 +234,16 @@ __device__ __forceinline__ void write_kept(const TokenRange& range, const Thresh
             kept[e] = __ballot(mine[e]);
             j += lanes_below(kept[e]);
         }
-        while (round <= R && start[round] < p0 + kChunk) {
-            const int in = start[round] - p0, in_lane = in >> 2, in_e = in & 3;
-            int under = at;
+        for (int starts = 64; starts == 64; round += starts) {  // a lane each (many: rounds of a few tokens, and those behind the last)
+            const int in = start[min(round + lane, R)] - p0, in_lane = in >> 2, in_e = in & 3;
+            const bool here = round + lane <= R && in < kChunk;
+            if (here) {
+                int under = at;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) under += __popcll(kept[e] & ((1ull << in_lane) - 1)) + (e < in_e && (kept[e] >> in_lane & 1));
-            if (lane == 0) below(round, under);
-            ++round;
+                for (int e = 0; e < 4; ++e) under += __popcll(kept[e] & ((1ull << in_lane) - 1)) + (e < in_e && (kept[e] >> in_lane & 1));
+                below(round + lane, under);
+            }
+            starts = __popcll(__ballot(here));
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -294,7 +296,7 @@ __global__ __launch_bounds__(kSelThreads) void select_tokens_kernel(SelectTokens
     const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const float* w = a.weights + (size_t)b * a.n_pos;
     if (tid == 0) s_count = 0;
-    for (int i = tid; i < kBins; i += kSelThreads) *reinterpret_cast<int4*>(&d.hist[4 * i]) = make_int4(0, 0, 0, 0);
+    clear_counts(d);
     const TokenRange range(a, round_starts(a, b, s_start, s_wave[0]));
     if (tid < kSelWaves) s_wave[tid][0] = s_wave[tid][1] = 0;
     __syncthreads();
@@ -311,6 +313,7 @@ __global__ __launch_bounds__(kSelThreads) void select_tokens_kernel(SelectTokens
         int left = d.left;
         const bool in_lds = d.here <= kCandidates;
         clear_counts(d);
+        __syncthreads();
         if (in_lds) {
             int sure = 0;
             each_chunk(held, w, range.n, c_lo, c_hi, [&](int p0, const float (&x)[4]) {
@@ -338,6 +341,7 @@ __global__ __launch_bounds__(kSelThreads) void select_tokens_kernel(SelectTokens
             t.key |= d.digit << kShift2;
             left = d.left;
             clear_counts(d);
+            __syncthreads();
             for (int i = tid; i < n_cand; i += kSelThreads)
                 if (s_cand[i].x >> kShift2 == t.key >> kShift2) count_bin(d.hist, s_cand[i].x & ((1 << kShift2) - 1));
             __syncthreads();
@@ -360,6 +364,7 @@ __global__ __launch_bounds__(kSelThreads) void select_tokens_kernel(SelectTokens
             t.key |= d.digit << kShift2;
             left = d.left;
             clear_counts(d);
+            __syncthreads();
             count_digit<3>(d, range, held, w, c_lo, c_hi, t.key);
             __syncthreads();
             find_digit<kShift2>(d, left);
@@ -418,6 +423,8 @@ struct SelectParts {
         s.n = (n_pos + s.chunks * kChunk - 1) / (s.chunks * kChunk);
         return s;
     }
+    // A wave's share begins with this chunk, wherever the sequence ends, so that its weights are asked for before that is known.
+    __device__ int first_chunk(int part, int wave) const { return part * chunks + chunks * wave / kSelWaves; }
     __device__ int used(int positions) const { return (positions + chunks * kChunk - 1) / (chunks * kChunk); }  // parts with positions
     __host__ __device__ size_t scratch() const { return (size_t)n * (2 * kBins + (1 << kShift2) + 2) + 4; }  // numbers
 };
@@ -477,14 +484,14 @@ __global__ __launch_bounds__(kSelThreads) void select_count_kernel(SelectTokensA
     __shared__ __align__(16) DigitCounts d;
     __shared__ int s_start[kMaxRounds + 1], s_wave[kSelWaves];
     const int part = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const float* w = a.weights + (size_t)b * a.n_pos;
+    const int c_lo = parts.first_chunk(part, wave);
+    const Chunks held = load_chunks(w, a.n_pos, c_lo, parts.first_chunk(part, wave + 1));
+    clear_counts(d);
     const TokenRange range(a, round_starts(a, b, s_start, s_wave));
-    const int used = parts.used(range.n);
+    const int used = parts.used(range.n), c_hi = min(parts.first_chunk(part, wave + 1), (range.n + kChunk - 1) / kChunk);
     if (part >= used) return;
     const SelectScratch at(a, b, parts.n);
-    const float* w = a.weights + (size_t)b * a.n_pos;
-    const int c0 = part * parts.chunks, chunks = max(min((range.n + kChunk - 1) / kChunk - c0, parts.chunks), 0);
-    const int c_lo = c0 + chunks * wave / kSelWaves, c_hi = c0 + chunks * (wave + 1) / kSelWaves;
-    const Chunks held = load_chunks(w, range.n, c_lo, c_hi);  // (on their way while the counts before are added up)
     uint32_t key = 0;
     if constexpr (LEVEL > 1) {
         const uint32_t digit1 = LEVEL == 3 ? (uint32_t)at.found[0] : 0;
@@ -500,7 +507,6 @@ __global__ __launch_bounds__(kSelThreads) void select_count_kernel(SelectTokensA
         const int above = block_sum(((uint32_t)thread_digit<2>(0) > digit ? mine[0] : 0) + ((uint32_t)thread_digit<2>(1) > digit ? mine[1] : 0), s_wave);
         if (tid == 0) at.above[2 * part + LEVEL - 2] = above;
     }
-    clear_counts(d);
     count_digit<LEVEL>(d, range, held, w, c_lo, c_hi, key);
     __syncthreads();
     constexpr int kCounts = LEVEL == 3 ? 1 << kShift2 : kBins;
@@ -513,9 +519,11 @@ __global__ __launch_bounds__(kSelThreads) void select_write_kernel(SelectTokensA
     __shared__ __align__(16) DigitCounts d;
     __shared__ int s_start[kMaxRounds + 1], s_wave[kSelWaves], s_sure[kSelWaves], s_ties[kSelWaves];
     const int part = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const float* w = a.weights + (size_t)b * a.n_pos;
+    const int c_lo = parts.first_chunk(part, wave);
+    const Chunks held = load_chunks(w, a.n_pos, c_lo, parts.first_chunk(part, wave + 1));
     const TokenRange range(a, round_starts(a, b, s_start, s_wave));
     const SelectScratch at(a, b, parts.n);
-    const float* w = a.weights + (size_t)b * a.n_pos;
     int32_t* idx = a.kept_idx + (size_t)b * a.budget;
     fill(idx + range.K, a.budget - range.K, (int32_t)-1, part * kSelThreads + tid, parts.n * kSelThreads);
     int32_t* below = a.kept_len + (size_t)b * a.R_max;
@@ -524,9 +532,7 @@ __global__ __launch_bounds__(kSelThreads) void select_write_kernel(SelectTokensA
             if (s_start[r] >= (range.n + kChunk - 1) / kChunk * kChunk) below[r] = range.K;
     const int used = parts.used(range.n);
     if (part >= used) return;
-    const int c0 = part * parts.chunks, chunks = max(min((range.n + kChunk - 1) / kChunk - c0, parts.chunks), 0), p0 = min(c0 * kChunk, range.n);
-    const int c_lo = c0 + chunks * wave / kSelWaves, c_hi = c0 + chunks * (wave + 1) / kSelWaves;
-    const Chunks held = load_chunks(w, range.n, c_lo, c_hi);
+    const int c_hi = min(parts.first_chunk(part, wave + 1), (range.n + kChunk - 1) / kChunk), p0 = part * parts.chunks * kChunk;
     int mine[1], before[1];
     add_parts(d, at.count3, used, part, at.found[3], mine, before);
     const uint32_t digit3 = d.digit;

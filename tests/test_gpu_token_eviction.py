@@ -178,6 +178,20 @@ def test_selection_by_several_workgroups(kind, budget, first, last):
     check_selection(w, lens, n_rounds, budget, first, last, block_size=16 if first else 0, stride=200000)
 
 
+@pytest.mark.parametrize("n_pos,most", [(9000, 8191), (80000, 70001), (80000, 65536)])
+def test_selection_of_many_rounds_that_begin_together(n_pos, most):
+    """Hundreds of empty rounds at one position: before, between and behind the others; weights behind the last token are NaN."""
+    rng = np.random.default_rng(most)
+    lens = np.zeros((3, 1000), dtype=np.int32)
+    lens[0, 70:140] = rng.multinomial(most, np.ones(70) / 70)
+    lens[1, [0, 1, 500, 999]] = [256, 3, 300, 40]
+    lens[2, :500] = 1
+    w = rng.lognormal(0, 2, (3, n_pos)).astype(np.float32)
+    for b in range(3):
+        w[b, lens[b].sum():] = np.nan
+    check_selection(w, lens, np.array([1000, 1000, 700]), 4000, 5, 70, stride=100000)
+
+
 def test_positions_behind_the_weights_are_not_there():
     w = np.linspace(0, 1, 50, dtype=np.float32)[None].repeat(2, 0)
     check_selection(w, np.array([[30, 40, 5], [10, 10, 10]], dtype=np.int32), np.array([3, 3]), 20, 3, 5)
