@@ -19,7 +19,7 @@
 //
 // P is rounded to bf16 twice (P = hi + lo, both bf16) so that the product carries ~16 bits of P; with 64 channels three
 // times (hi + mid + lo: all 24 bits), since those calls used to run on the vector ALU in fp32 and the matrix cores have
-// the time (half the products per token).
+// the time (half the products per token), and for a tree of drafted tokens, whose outputs are as exact as the fp32 form's.
 //
 // Work decomposition (range_schedule.hpp): the key tiles of the whole batch are cut into equal ranges, and ONE
 // WAVEFRONT streams one range for one (KV head, block of 16 query rows), two tiles in flight, everything it

@@ -541,12 +541,13 @@ static int tree_attention(ra_ctx* ctx, hipStream_t st, AttnArgs& a, bool bf16) {
     const int64_t max_tokens = a.max_tokens + a.cur_cap;
     RA_REQUIRE(max_tokens < (int64_t)1 << 30, RA_ERR_UNSUPPORTED, "tree: max_tokens too large");
     const size_t rows = (size_t)B * rows_total * Hkv;
-    a.min_units = bf16 ? 8 : 2;  // (fp32 calls are small: one dialogue of 500 tokens)
-    a.S = tree_pieces(inner * B, (long long)kTreeWaves * ctx->num_cu, max_tokens / kUnitTokens, a.min_units);
-    AttnWorkspace w = attn_workspace(rows, a.S, D, B, a.view.R_max);
-    while (a.S > 1 && w.total > ctx->ws.bytes) w = attn_workspace(rows, --a.S, D, B, a.view.R_max);
+    AttnWorkspace w = attn_workspace(rows, 1, D, B, a.view.R_max);
     RA_REQUIRE(ctx->ws.base != nullptr && ctx->ws.bytes >= w.total, RA_ERR_WORKSPACE,
                "tree: workspace has %zu bytes, this call needs %zu", ctx->ws.bytes, w.total);
+    a.min_units = bf16 ? 8 : 2;  // (fp32 calls are small: one dialogue of 500 tokens)
+    a.S = tree_pieces(inner * B, (long long)kTreeWaves * ctx->num_cu, max_tokens / kUnitTokens, a.min_units);
+    w = attn_workspace(rows, a.S, D, B, a.view.R_max);
+    while (a.S > 1 && w.total > ctx->ws.bytes) w = attn_workspace(rows, --a.S, D, B, a.view.R_max);
     a.part_acc = reinterpret_cast<float*>(ctx->ws.base + w.acc_off);
     a.part_m = reinterpret_cast<float*>(ctx->ws.base + w.m_off);
     a.part_l = reinterpret_cast<float*>(ctx->ws.base + w.l_off);

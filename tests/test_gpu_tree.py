@@ -68,9 +68,9 @@ def run_tree(lens, Hkv, G, d, dtype, n, cap, paged, kind="tree", seed=0, select=
         T = k.shape[1]
         sees = np.ones((m, T), dtype=bool)
         sees[:, T - m:] = bits[b, :m, :m]
-        # bf16: a weight goes to the matrix cores as two bf16 numbers cut off, of 8 bits each: relative error below 2^-14;
-        # sums of T weights and of their products with the values in fp32
-        rounding = (2.0 ** -14 if dtype == "bf16" else 0.0) + 2 * unit_roundoff_sum(T + 64)
+        # bf16: a weight goes to the matrix cores as three bf16 numbers, which hold all of its bits: 3 T products are added up in
+        # fp32, T weights, and what is merged
+        rounding = 4 * unit_roundoff_sum(T + 64)
         for h in range(Hq):
             g = h // G
             s = np.where(sees, q[b, :m, h] @ k[g].T * scale_of(d), -np.inf)
