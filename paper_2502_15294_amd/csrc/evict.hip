@@ -29,8 +29,7 @@ constexpr int kDigit = 11, kBins = 1 << kDigit;  // three digits: 11, 11 and 10 
 constexpr int kChunk = 256;                      // positions that a wave reads with one instruction: four a lane
 constexpr int kChunks = 8;                       // ... that it has in flight
 constexpr int kCandidates = 8192;                // keys that share the first digit with the threshold and fit into LDS
-constexpr int kManyPositions = 65536;            // positions from which several workgroups take a sequence (60 000: 39.7 microseconds and
-                                                 // 37.7 by one; 80 000: 40 and 45; 236 000: 55 and 106)
+constexpr int kManyPositions = 65536;            // positions from which several workgroups take a sequence (SelectParts)
 
 typedef float float4_any __attribute__((ext_vector_type(4), aligned(4)));
 
@@ -413,21 +412,29 @@ __global__ __launch_bounds__(kSelThreads) void select_tokens_kernel(SelectTokens
 // Every workgroup has a part of the positions.  Three launches count the digits, each of them adding up what the one before
 // counted in all parts; one writes the kept positions, every part behind what the parts before it keep; the last one writes
 // the rounds and the weights.  Until then the counts lie where those weights will: kept_weights holds them (5120 numbers a part
-// of 16384 positions or more, from two parts on).
-constexpr int kPartPositions = 16384;  // (with 8192: 16 dialogues of 131 000 tokens 71 microseconds instead of 60; with 32768: 74)
+// of 8192 positions or more).
+constexpr int kPartPositions = 8192;
+constexpr int kMinParts = 8, kMaxParts = 64;  // (each adds up the counts of all)
 struct SelectParts {
     int n, chunks;  // parts; chunks of a part
-    __host__ __device__ static SelectParts of(int n_pos) {
+    // No more parts than compute units, which such a workgroup fills: twice as many took 78 microseconds instead of 51 (16 dialogues of
+    // 131 000 tokens).  Where that leaves a sequence fewer than eight it is one workgroup's (64 dialogues of 48 000 tokens: 47, four
+    // parts 58; 100 of 131 000: 122, two parts 170), and so are short sequences: one of 48 000 tokens 44, parts of 16384 positions
+    // 39.6, of 8192 34.5; of 36 000 36 and 34; of 30 000 30 and 33.
+    static bool pays(int n_pos, int B, int num_cu) { return n_pos >= kManyPositions && B <= num_cu / kMinParts; }
+    static SelectParts of(int n_pos, int B, int num_cu) {
+        const int most = num_cu / B < kMaxParts ? num_cu / B : kMaxParts;
         SelectParts s;
-        s.chunks = kPartPositions / kChunk * ((n_pos + 64 * kPartPositions - 1) / (64 * kPartPositions));  // 64 parts at most: each adds up the counts of all
+        s.chunks = kPartPositions / kChunk * ((n_pos - 1) / kPartPositions / most + 1);
         s.n = (n_pos + s.chunks * kChunk - 1) / (s.chunks * kChunk);
         return s;
     }
     // A wave's share begins with this chunk, wherever the sequence ends, so that its weights are asked for before that is known.
     __device__ int first_chunk(int part, int wave) const { return part * chunks + chunks * wave / kSelWaves; }
     __device__ int used(int positions) const { return (positions + chunks * kChunk - 1) / (chunks * kChunk); }  // parts with positions
-    __host__ __device__ size_t scratch() const { return (size_t)n * (2 * kBins + (1 << kShift2) + 2) + 4; }  // numbers
 };
+constexpr int kPartNumbers = 2 * kBins + (1 << kShift2) + 2;
+static_assert(kPartNumbers <= kPartPositions && (kManyPositions / kPartPositions + 1) * kPartNumbers + 4 <= kManyPositions, "they fit");
 struct SelectScratch {
     int *count1, *count2, *count3;  // [parts][bins]
     int* found;                     // digit and what is left, of the first and the second level
@@ -861,8 +868,8 @@ extern "C" int ra_select_tokens(ra_ctx* ctx, void* stream, const float* weights,
     a.kept_off = reinterpret_cast<long long*>(kept_off);
     a.kept_weights = kept_weights;
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-    const SelectParts parts = SelectParts::of(n_pos);
-    if (kept_weights != nullptr && n_pos >= kManyPositions && parts.scratch() <= (size_t)n_pos && B <= 65535) {
+    if (kept_weights != nullptr && SelectParts::pays(n_pos, B, ctx->num_cu)) {
+        const SelectParts parts = SelectParts::of(n_pos, B, ctx->num_cu);
         const dim3 grid((unsigned)parts.n, (unsigned)B), block(kSelThreads);
         hipLaunchKernelGGL((select_count_kernel<1>), grid, block, 0, st, a, parts);
         hipLaunchKernelGGL((select_count_kernel<2>), grid, block, 0, st, a, parts);

@@ -178,6 +178,15 @@ def test_selection_by_several_workgroups(kind, budget, first, last):
     check_selection(w, lens, n_rounds, budget, first, last, block_size=16 if first else 0, stride=200000)
 
 
+@pytest.mark.parametrize("B,n_pos", [(32, 70000), (33, 66000), (1, 2_700_000)])
+def test_selection_of_large_batches_and_very_long_sequences(B, n_pos):
+    """The most sequences of several workgroups each, one more, and parts of which a wave does not hold all weights at once."""
+    rng = np.random.default_rng(B)
+    lens = rng.multinomial(n_pos - 1000, np.ones(900) / 900, size=B).astype(np.int32)
+    w = rng.lognormal(0, 2, (B, n_pos)).astype(np.float32)
+    check_selection(w, lens, np.full(B, 900), n_pos // 4, 16, 1000, stride=n_pos)
+
+
 @pytest.mark.parametrize("n_pos,most", [(9000, 8191), (80000, 70001), (80000, 65536)])
 def test_selection_of_many_rounds_that_begin_together(n_pos, most):
     """Hundreds of empty rounds at one position: before, between and behind the others; weights behind the last token are NaN."""
