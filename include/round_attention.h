@@ -364,7 +364,7 @@ int ra_round_sparse_attn_tree(ra_ctx* ctx, void* stream, const void* q, int n_no
  *   path       device int32 [B][max_path]: node indices in the order of the path.  A tree numbers its nodes behind their
  *              parents, so path[b][j] >= j.  The path ends before the first entry that is smaller than j or whose row lies
  *              outside cur_k, and after n_path[b] entries at the latest (device int32 [B], clamped to 0 .. max_path)
- *   new_len    device int32 [B], another buffer than cur_len
+ *   new_len    device int32 [B], another buffer than cur_len, path and n_path
  * Rows behind the path keep what they held.  Needs Hkv * d * element size to be a multiple of 16 bytes
  * (RA_ERR_UNSUPPORTED otherwise).  No workspace is used.
  */
@@ -410,7 +410,8 @@ typedef struct ra_keep_params {
  *   weights    device float [B][n_pos], not NaN;  positions n_pos and above count as not there
  *   seg_len    device int32 [B][R_max], n_rounds device int32 [B]: those of the view
  *   kept_idx   device int32 [B][budget]: positions of the kept tokens, ascending, -1 behind the last;  n_kept device int32 [B]
- *   kept_len   device int32 [B][R_max]: tokens that every round keeps (0 from n_rounds[b] on): seg_len of the smaller cache
+ *   kept_len   device int32 [B][R_max]: tokens that every round keeps (0 from n_rounds[b] on): seg_len of the smaller cache.
+ *              kept_len and n_kept are other buffers than seg_len and n_rounds
  *   kept_off   device int64 [B][R_max] or NULL: a place for every round, packed in whole 16-token blocks behind b * stride,
  *              in tokens (seg_off and seg_off_v of a contiguous cache) or slots (seg_off of a paged one)
  *   kept_weights   device float [B][n_pos] or NULL: the kept tokens' weights at their new positions, 0 behind the last;

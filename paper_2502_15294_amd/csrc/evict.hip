@@ -833,6 +833,10 @@ static int compact_piece(int64_t tokens, int num_cu) {
 
 using namespace ra;
 
+static bool overlap(const void* a, size_t a_bytes, const void* b, size_t b_bytes) {
+    return a != nullptr && (uintptr_t)a < (uintptr_t)b + b_bytes && (uintptr_t)b < (uintptr_t)a + a_bytes;
+}
+
 extern "C" int ra_select_tokens(ra_ctx* ctx, void* stream, const float* weights, int n_pos, const int32_t* seg_len,
                                 const int32_t* n_rounds, int B, int R_max, const ra_keep_params* params, int32_t* kept_idx,
                                 int32_t* n_kept, int32_t* kept_len, int64_t* kept_off, float* kept_weights) {
@@ -850,7 +854,11 @@ extern "C" int ra_select_tokens(ra_ctx* ctx, void* stream, const float* weights,
     RA_REQUIRE(params->stride >= 0, RA_ERR_INVALID_ARG, "select_tokens: stride is negative");
     RA_REQUIRE(weights && seg_len && n_rounds && kept_idx && n_kept && kept_len, RA_ERR_INVALID_ARG,
                "select_tokens: NULL argument");
-    RA_REQUIRE(kept_weights != weights, RA_ERR_INVALID_ARG, "select_tokens: kept_weights must be another buffer than weights");
+    const size_t weight_bytes = (size_t)B * n_pos * sizeof(float), round_bytes = (size_t)B * R_max * sizeof(int32_t);
+    RA_REQUIRE(!overlap(kept_weights, weight_bytes, weights, weight_bytes), RA_ERR_INVALID_ARG,
+               "select_tokens: kept_weights must be another buffer than weights");
+    RA_REQUIRE(!overlap(kept_len, round_bytes, seg_len, round_bytes) && n_kept != n_rounds, RA_ERR_INVALID_ARG,
+               "select_tokens: kept_len and n_kept must be other buffers than seg_len and n_rounds");
     SelectTokensArgs a = {};
     a.weights = weights;
     a.seg_len = seg_len;

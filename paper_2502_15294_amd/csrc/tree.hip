@@ -674,7 +674,8 @@ extern "C" int ra_tree_commit(ra_ctx* ctx, void* stream, void* const* cur_k_laye
                "tree_commit: non-positive dimension");
     RA_REQUIRE(cur_k_layers && cur_v_layers && cur_len && path && n_path && new_len, RA_ERR_INVALID_ARG, "tree_commit: NULL argument");
     RA_REQUIRE(dtype == RA_F32 || dtype == RA_BF16, RA_ERR_UNSUPPORTED, "tree_commit: unknown dtype %d", dtype);
-    RA_REQUIRE(new_len != cur_len, RA_ERR_INVALID_ARG, "tree_commit: new_len must be another buffer than cur_len");
+    RA_REQUIRE(new_len != cur_len && new_len != n_path && (new_len < path || new_len >= path + (size_t)B * max_path), RA_ERR_INVALID_ARG,
+               "tree_commit: new_len must be another buffer than cur_len, path and n_path");
     const long long row_bytes = (long long)Hkv * d * (dtype == RA_BF16 ? 2 : 4);
     RA_REQUIRE(row_bytes % 16 == 0, RA_ERR_UNSUPPORTED, "tree_commit: a token's %lld bytes are no multiple of 16", row_bytes);
     const long long columns = (row_bytes / 16 + 255) / 256;

@@ -101,7 +101,9 @@ def test_commit_refuses():
     call = ra.ra_tree_commit
     assert "NULL" in refused(BAD, call, None, **ok)
     same = i32(2)
-    assert "another buffer" in refused(BAD, call, CTX, **{**ok, "cur_len": same, "new_len": same})
+    for name in ("cur_len", "n_path"):
+        assert "another buffer" in refused(BAD, call, CTX, **{**ok, name: same, "new_len": same})
+    assert "another buffer" in refused(BAD, call, CTX, **{**ok, "new_len": ok["path"].flatten()[2:4]})
     assert "positive" in refused(BAD, call, CTX, **{**ok, "path": i32(2, 0)})
     refused(BAD, call, CTX, **{**ok, "path": None})
     assert "aligned" in refused(BAD, call, CTX, **{**ok, "cur_v_layers": [v[0], misaligned(v[1])]})
@@ -151,6 +153,10 @@ def test_selection_refuses():
     assert "R_max" in refused(NOT_MADE, call, CTX, **{**ok, "seg_len": i32(2, 1025)})
     assert "positive" in refused(BAD, call, CTX, **{**ok, "seg_len": i32(2, 0)})
     assert "another buffer" in refused(BAD, call, CTX, **{**ok, "kept_weights": ok["weights"]})
+    both = torch.zeros(3, 40)
+    assert "another buffer" in refused(BAD, call, CTX, **{**ok, "weights": both[:2], "kept_weights": both[1:]})
+    assert "other buffers" in refused(BAD, call, CTX, **{**ok, "kept_len": ok["seg_len"]})
+    assert "other buffers" in refused(BAD, call, CTX, **{**ok, "n_kept": ok["n_rounds"]})
     assert "2^24" in refused(NOT_MADE, call, CTX, torch.zeros(1, (1 << 24) + 1), i32(1, 3), i32(1), 10)
     for change in (dict(seg_len=torch.zeros(2, 3)), dict(n_rounds=i32(3)), dict(weights=torch.zeros(40)), dict(weights=torch.zeros(2, 40).half()),
                    dict(kept_idx=i32(2, 9)), dict(kept_off=i32(2, 3))):
