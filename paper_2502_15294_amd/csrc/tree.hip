@@ -310,9 +310,9 @@ __global__ __launch_bounds__(256, kTreeWaves) void tree_rows_kernel(AttnArgs a, 
         if (k_tokens == 16 || (PAGED && k_tokens < 32)) {  // whole rows 256 bytes apart (a block has 16 of them in any case)
             const long long base = k0 + q4 * 256 + key_chunk;
             load_to_lds_at<0>(base, kd);
-            load_to_lds_at<1024>(base, kd + 4096);
-            load_to_lds_at<2048>(base, kd + 8192);
-            load_to_lds_at<3072>(base, kd + 12288);
+            load_to_lds_at<1 * 1024>(base, kd + 4096);
+            load_to_lds_at<2 * 1024>(base, kd + 8192);
+            load_to_lds_at<3 * 1024>(base, kd + 12288);
         } else {
             const long long stride = k_tokens >= 32 ? (long long)Hkv * 256 : 256;
             const int last = (k_tokens & 31) - 1;
@@ -325,9 +325,9 @@ __global__ __launch_bounds__(256, kTreeWaves) void tree_rows_kernel(AttnArgs a, 
         if (!__any(v_tokens >= 32)) {
             const long long base = v0 + wave * 1024 + n * 32;
             load_to_lds_at<0>(base, vd);
-            load_to_lds_at<16>(base, vd + 1024);
-            load_to_lds_at<512>(base, vd + 2048);
-            load_to_lds_at<528>(base, vd + 3072);
+            load_to_lds_at<16>(base, vd + 1 * 1024);
+            load_to_lds_at<512>(base, vd + 2 * 1024);
+            load_to_lds_at<528>(base, vd + 3 * 1024);
         } else {
             p.some = true;
             const int last = (v_tokens & 31) - 1;
